@@ -498,6 +498,122 @@ HETEGEN_API hetegen_status hetegen_model_kv_read(hetegen_ctx* ctx, hetegen_model
 HETEGEN_API hetegen_status hetegen_decode_step_kv(hetegen_ctx* ctx, hetegen_model* model, const void* x_dev,
                                                   void* out_dev, int B, int pos, void* stream);
 
+/* ---- Paged KV cache ----
+ * A cache for sequences of different lengths: n_pages pages of page_size positions, in one
+ * device buffer of the caller's, and a table that names each sequence's pages.  Values are kept
+ * in the activation type or in 8 bits with one binary32 scale for each token and head, keys and
+ * values apart.  The calls below write new tokens into it, read positions back, and let new
+ * tokens (one, or a chunk of a prompt) attend to it; hetegen_decode_step_paged runs a decode
+ * step over it.  They allocate nothing, read nothing from the device and wait for nothing, so
+ * they can be captured into a HIP graph: the lengths and the table are read when the kernels
+ * run.  Calls that share no buffer they write may overlap, on any streams (a context still
+ * takes one call at a time from the host).
+ *
+ * Pages: record (page, head) holds record_bytes = hetegen_paged_kv_bytes / (n_pages * heads)
+ * bytes at (page * heads + head) * record_bytes: the keys of page_size positions, the values,
+ * and in 8-bit formats page_size binary32 scales of the keys and page_size of the values.
+ * Keys and values stand in the operand order of 16x16x32 matrix-core products (1 KiB = 64 pieces
+ * of 16 bytes, piece l = 16 g + i):
+ *   keys    per 16 positions, per 32 dimensions d0 (8 bits: 64): piece l is position i,
+ *           dimensions d0 + 8 g + [0, 8) (8 bits: these, then d0 + 32 + 8 g + [0, 8));
+ *   values  per 32 positions, per 16 dimensions d0 (8 bits: 32): piece l is dimension d0 + i,
+ *           positions 16 (e / 4) + 4 g + e % 4, e < 8 (8 bits: these, then those of
+ *           dimension d0 + 16 + i).
+ * Pages need no initialisation: what stands at a sequence's kv_len and behind does not reach results. */
+
+typedef enum {
+  HETEGEN_KV_SAME = 0, /* values as they are, in the cache's dtype */
+  HETEGEN_KV_I8 = 1,   /* code = round(x / c), half to even, c = max |x| / 127 over the head */
+  HETEGEN_KV_E4M3 = 2  /* OCP e4m3 of x / c, c = max |x| / 448 */
+} hetegen_kv_format;
+
+typedef struct {
+  int heads;                /* key/value heads, in [1, 1024] */
+  int head_dim;             /* 64 or 128 */
+  int page_size;            /* positions per page: 32, 64, 128 or 256 */
+  int n_pages;              /* >= 1 */
+  hetegen_dtype dtype;      /* of k, v, q and out: HETEGEN_F16 or HETEGEN_BF16 */
+  hetegen_kv_format format;
+} hetegen_paged_kv;
+
+/* The tokens of a call.  Rows [new_start[s], new_start[s + 1]) of k, v, q and out are the newest
+ * tokens of sequence s, in order, and kv_len[s] is the number of its positions with them: row
+ * new_start[s] + i is position kv_len[s] - n + i, n = new_start[s + 1] - new_start[s] >= 0.
+ * Position j lies in page page_table[s * max_pages + j / page_size]; an entry outside
+ * [0, n_pages) names no page.  new_start does not decrease; rows before new_start[0], behind
+ * new_start[n_seq] and past max_new tokens of a sequence are left as they were.  Device
+ * arrays, 4-byte aligned; whatever they hold, nothing outside the rows, the table and the pages is
+ * read or written.  One sequence's pages may be another's, too (a common beginning), but for
+ * pages that a write of the same call goes to. */
+typedef struct {
+  int n_tokens;              /* rows, in [0, 2^22]; n_tokens * heads < 2^28 */
+  int n_seq;                 /* in [0, 2^20] */
+  int max_new;               /* most new tokens of any sequence, >= 1 */
+  int max_pages;             /* columns of the table, >= 1; max_pages * page_size <= 2^30 */
+  const int32_t* new_start;  /* [n_seq + 1] */
+  const int32_t* kv_len;     /* [n_seq] */
+  const int32_t* page_table; /* [n_seq, max_pages] */
+} hetegen_paged_batch;
+
+/* Bytes of a cache's pages (16-byte aligned device memory), 0 for a description that the calls
+ * below refuse. */
+HETEGEN_API size_t hetegen_paged_kv_bytes(const hetegen_paged_kv* kv);
+
+/* Write the tokens' keys and values k_dev, v_dev [n_tokens, heads * head_dim] (device, kv->dtype,
+ * row stride ld elements, ld % 8 == 0, 16-byte aligned: slices of a qkv output, for instance).
+ * Positions below 0 and positions without a page are not written.  A row (token and head) with
+ * an infinity or a NaN in it is kept in 8 bits as NaN throughout.  Enqueued on `stream`. */
+HETEGEN_API hetegen_status hetegen_paged_kv_write(hetegen_ctx* ctx, const hetegen_paged_kv* kv, void* pages_dev,
+                                                  const hetegen_paged_batch* batch, const void* k_dev,
+                                                  const void* v_dev, long long ld, void* stream);
+
+/* Read positions back: rows as in hetegen_paged_kv_write, 8-bit codes times their scale, rounded
+ * once to kv->dtype.  Rows of positions without a page are zeros; rows of positions below 0 are
+ * left as they were.  k_dev and v_dev may not overlap. */
+HETEGEN_API hetegen_status hetegen_paged_kv_read(hetegen_ctx* ctx, const hetegen_paged_kv* kv, const void* pages_dev,
+                                                 const hetegen_paged_batch* batch, void* k_dev, void* v_dev,
+                                                 long long ld, void* stream);
+
+/* Bytes of workspace for hetegen_paged_attention with these sizes (`heads` query heads; the
+ * batch's pointers are not read), 0 for arguments it refuses.  Does not shrink as n_tokens, n_seq,
+ * max_new or max_pages grow, so one workspace serves every call up to the largest. */
+HETEGEN_API size_t hetegen_paged_attention_ws_bytes(const hetegen_paged_kv* kv, const hetegen_paged_batch* batch,
+                                                    int heads);
+
+/* Attention of the batch's tokens over the cache, which holds them already (hetegen_paged_kv_write):
+ *   out[t, h] = sum_j softmax(scale * q[t, h] . K_j)_j V_j over the positions j in [0, position of t]
+ * that have a page, K and V of key/value head h / (heads / kv->heads); 0 where there is none.
+ * q_dev and out_dev [n_tokens, heads * head_dim] (device, kv->dtype, row strides ldq and ldo
+ * elements, multiples of 8, 16-byte aligned, not overlapping).  heads is a multiple of kv->heads, at
+ * most 1024; scale is finite (1 / sqrt(head_dim) as a rule).  Softmax and sums in binary32; keys
+ * and values in masked places do not reach the result, whatever they are.
+ * ws_dev: hetegen_paged_attention_ws_bytes of device memory, 16-byte aligned, of which the first
+ * 256 KiB are zero before its first use (every call leaves them zero); calls that overlap need a
+ * workspace each.  Results do not depend on timing; their last bits may depend on the batch's sizes
+ * (how rows are dealt to kernels and how many workgroups share a sequence).  Enqueued on `stream`. */
+HETEGEN_API hetegen_status hetegen_paged_attention(hetegen_ctx* ctx, const hetegen_paged_kv* kv, const void* pages_dev,
+                                                   const hetegen_paged_batch* batch, int heads, const void* q_dev,
+                                                   long long ldq, void* out_dev, long long ldo, double scale,
+                                                   void* ws_dev, size_t ws_bytes, void* stream);
+
+/* Bytes of workspace for hetegen_decode_step_paged (the attention's, and its output); 0 for
+ * arguments it refuses. */
+HETEGEN_API size_t hetegen_decode_step_paged_ws_bytes(const hetegen_model* model, const hetegen_paged_kv* kv,
+                                                      const hetegen_paged_batch* batch);
+
+/* A decode step of the batch's tokens over a paged cache: as hetegen_decode_step_kv with
+ * B = n_tokens rows (at most the model's max_batch) x_dev -> out_dev, which may be one token of
+ * each of several sequences, or several of one (a prompt in pieces, proposed tokens).  Each layer
+ * writes its keys and values to the cache and attends to it (scale 1 / sqrt(head_dim)).
+ * pages_dev: the model's layers one after another, L * hetegen_paged_kv_bytes(kv) bytes;
+ * kv->heads * kv->head_dim is the model's hidden size, kv->dtype its type.  Independent of
+ * hetegen_model_kv_create.  Rows of out_dev that belong to no sequence are undefined.  ws_dev as in
+ * hetegen_paged_attention. */
+HETEGEN_API hetegen_status hetegen_decode_step_paged(hetegen_ctx* ctx, hetegen_model* model,
+                                                     const hetegen_paged_kv* kv, void* pages_dev,
+                                                     const hetegen_paged_batch* batch, const void* x_dev,
+                                                     void* out_dev, void* ws_dev, size_t ws_bytes, void* stream);
+
 /* Optional trace of every linear's input and output (model dtype), for
  * teacher-forced checks.  Linear i writes its input [B, K_i] and then its output
  * [B, N_i] (after the fused ReLU or residual sum), packed in order of i; the

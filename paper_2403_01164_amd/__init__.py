@@ -25,6 +25,7 @@ OK, ERR_INVALID_ARG, ERR_NOT_PINNED, ERR_UNSUPPORTED, ERR_OOM, ERR_HIP, ERR_INTE
 PLAN_APPROX = 1
 EXEC_AUTO, EXEC_PERSISTENT, EXEC_GRAPH, EXEC_EAGER = 0, 1, 2, 3
 BENCH_CROSSING, BENCH_WALL = 0, 1
+KV_SAME, KV_I8, KV_E4M3 = 0, 1, 2
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "NOT_PINNED", 3: "UNSUPPORTED", 4: "OOM", 5: "HIP", 6: "INTERNAL"}
 
 if not os.path.exists(LIB_PATH):
@@ -59,8 +60,22 @@ class Profile(ctypes.Structure):
         return {name: getattr(self, name) for name, _ in self._fields_}
 
 
+class PagedKV(ctypes.Structure):
+    """A paged cache's sizes, type and format (hetegen_paged_kv)."""
+    _fields_ = [("heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("n_pages", ctypes.c_int), ("dtype", ctypes.c_int), ("format", ctypes.c_int)]
+
+
+class PagedBatch(ctypes.Structure):
+    """The tokens of a call on a paged cache (hetegen_paged_batch); the last three are device addresses."""
+    _fields_ = [("n_tokens", ctypes.c_int), ("n_seq", ctypes.c_int), ("max_new", ctypes.c_int),
+                ("max_pages", ctypes.c_int), ("new_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p)]
+
+
 _lib = ctypes.CDLL(LIB_PATH)
 _vp, _i, _d, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_double, ctypes.c_size_t
+_ll, _kv, _batch = ctypes.c_longlong, ctypes.POINTER(PagedKV), ctypes.POINTER(PagedBatch)
 _SIGS = {
     "hetegen_create": ([ctypes.POINTER(Config), ctypes.POINTER(_vp)], _i),
     "hetegen_destroy": ([_vp], _i),
@@ -105,6 +120,13 @@ _SIGS = {
     "hetegen_model_trace_bytes": ([_vp, _i], _sz),
     "hetegen_model_set_trace": ([_vp, _vp, _sz], _i),
     "hetegen_model_destroy": ([_vp, _vp], _i),
+    "hetegen_paged_kv_bytes": ([_kv], _sz),
+    "hetegen_paged_kv_write": ([_vp, _kv, _vp, _batch, _vp, _vp, _ll, _vp], _i),
+    "hetegen_paged_kv_read": ([_vp, _kv, _vp, _batch, _vp, _vp, _ll, _vp], _i),
+    "hetegen_paged_attention_ws_bytes": ([_kv, _batch, _i], _sz),
+    "hetegen_paged_attention": ([_vp, _kv, _vp, _batch, _i, _vp, _ll, _vp, _ll, _d, _vp, _sz, _vp], _i),
+    "hetegen_decode_step_paged_ws_bytes": ([_vp, _kv, _batch], _sz),
+    "hetegen_decode_step_paged": ([_vp, _vp, _kv, _vp, _batch, _vp, _vp, _vp, _sz, _vp], _i),
     "hetegen_set_profiling": ([_vp, _i], _i),
     "hetegen_get_profile": ([_vp, ctypes.POINTER(Profile), _i], _i),
 }
@@ -426,3 +448,38 @@ def hetegen_probe_launch(ctx, reps=1000, stream=0):
     out = _d()
     _check(_lib.hetegen_probe_launch(ctx, reps, stream or None, ctypes.byref(out)), ctx)
     return out.value
+
+
+def hetegen_paged_kv_bytes(kv):
+    """Bytes of a cache's pages (kv: PagedKV), 0 if the calls refuse it."""
+    return _lib.hetegen_paged_kv_bytes(kv)
+
+
+def hetegen_paged_kv_write(ctx, kv, pages_dev, batch, k_dev, v_dev, ld, stream=0):
+    """Write the tokens of batch (PagedBatch), rows of k and v with stride ld elements, into the pages."""
+    _check(_lib.hetegen_paged_kv_write(ctx, kv, pages_dev, batch, k_dev, v_dev, ld, stream), ctx)
+
+
+def hetegen_paged_kv_read(ctx, kv, pages_dev, batch, k_dev, v_dev, ld, stream=0):
+    """Read the positions of batch's tokens back into rows of k and v."""
+    _check(_lib.hetegen_paged_kv_read(ctx, kv, pages_dev, batch, k_dev, v_dev, ld, stream), ctx)
+
+
+def hetegen_paged_attention_ws_bytes(kv, batch, heads):
+    return _lib.hetegen_paged_attention_ws_bytes(kv, batch, heads)
+
+
+def hetegen_paged_attention(ctx, kv, pages_dev, batch, heads, q_dev, ldq, out_dev, ldo, scale, ws_dev, ws_bytes,
+                            stream=0):
+    """Attention of batch's tokens over the cache that holds them; the workspace's first 256 KiB start as zeros."""
+    _check(_lib.hetegen_paged_attention(ctx, kv, pages_dev, batch, heads, q_dev, ldq, out_dev, ldo, scale, ws_dev,
+                                        ws_bytes, stream), ctx)
+
+
+def hetegen_decode_step_paged_ws_bytes(model, kv, batch):
+    return _lib.hetegen_decode_step_paged_ws_bytes(model, kv, batch)
+
+
+def hetegen_decode_step_paged(ctx, model, kv, pages_dev, batch, x_dev, out_dev, ws_dev, ws_bytes, stream=0):
+    _check(_lib.hetegen_decode_step_paged(ctx, model, kv, pages_dev, batch, x_dev, out_dev, ws_dev, ws_bytes,
+                                          stream), ctx)

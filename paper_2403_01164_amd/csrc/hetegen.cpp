@@ -44,6 +44,7 @@
 #include "cpu_share.h"
 #include "hbm_probe.h"
 #include "kernels.h"
+#include "paged.h"
 #include "pin_team.h"
 
 namespace {
@@ -1775,10 +1776,43 @@ hetegen_status run_attention(hetegen_ctx* ctx, hetegen_model* m, int l, int B, i
   return HETEGEN_OK;
 }
 
+// What a step over a paged cache needs beside the model.
+struct PagedStep {
+  hg::PagedCache kv;
+  hg::PagedSeqs seqs;
+  size_t layer_bytes;  // from one layer's pages to the next one's
+  void* ws;            // the attention's workspace
+  void* attn;          // attention output [n_tokens, H]
+};
+
+// Attention of layer l over its paged cache: writes k and v of the qkv buffer into it, then
+// attends with q; the output goes to p.attn.
+hetegen_status run_paged_attention(hetegen_ctx* ctx, hetegen_model* m, const PagedStep& p, int l, hipStream_t st) {
+  hg::PagedCopyParams w{};
+  w.kv = p.kv;
+  w.kv.pages = (char*)p.kv.pages + (size_t)l * p.layer_bytes;
+  w.seqs = p.seqs;
+  w.k = (uint16_t*)m->qkv + m->H;
+  w.v = (uint16_t*)m->qkv + 2 * (size_t)m->H;
+  w.ld = 3LL * m->H;
+  HIPCHK(ctx, hg::launch_paged_write(w, st));
+  hg::PagedAttnParams a{};
+  a.kv = w.kv;
+  a.seqs = p.seqs;
+  a.q = m->qkv;
+  a.ldq = 3LL * m->H;
+  a.out = p.attn;
+  a.ldo = m->H;
+  a.heads = p.kv.heads;
+  HIPCHK(ctx, hg::launch_paged_attention(a, 1.0 / sqrt((double)p.kv.head_dim), p.ws, st));
+  return HETEGEN_OK;
+}
+
 // One step.  pos < 0: the attention of every layer is that of an empty cache (the
-// value slice of qkv); pos >= 0: attention over the KV cache at position pos.
+// value slice of qkv); pos >= 0: attention over the KV cache at position pos; paged:
+// attention over a paged cache.
 hetegen_status enqueue_step(hetegen_ctx* ctx, hetegen_model* m, const void* x_dev, void* out_dev, int B,
-                            hipStream_t st, int pos = -1) {
+                            hipStream_t st, int pos = -1, const PagedStep* paged = nullptr) {
   const int H = m->H, F = m->F;
   // plan every streamed chunk of the step up front so the copy stream can run
   // ahead across linears and layers, bounded by the ring
@@ -1840,7 +1874,10 @@ hetegen_status enqueue_step(hetegen_ctx* ctx, hetegen_model* m, const void* x_de
           j.y = m->qkv; j.ldy = 3 * H; j.epi = hg::EPI_NONE;
           break;
         case 1:  // x = x + (A Wout^T + b): A = attention over the cache, or V = qkv[:, 2H:3H]
-          if (pos >= 0) {
+          if (paged) {
+            TRY(run_paged_attention(ctx, m, *paged, l, st));
+            j.x = paged->attn; j.ldx = H;
+          } else if (pos >= 0) {
             TRY(run_attention(ctx, m, l, B, pos, st));
             j.x = m->abuf; j.ldx = H;
           } else {
@@ -2636,6 +2673,231 @@ hetegen_status hetegen_decode_step_kv(hetegen_ctx* ctx, hetegen_model* m, const 
     HIPCHK(ctx, hipSetDevice(ctx->device));
     m->last_exec = HETEGEN_EXEC_EAGER;
     hetegen_status s = enqueue_step(ctx, m, x_dev, out_dev, B, (hipStream_t)stream, pos);
+    if (s != HETEGEN_OK) {
+      reset_pipeline(ctx);
+      return s;
+    }
+    return finish_call(ctx, t0);
+  });
+}
+
+}  // extern "C"
+
+// ---- paged KV cache ----
+namespace {
+
+constexpr int kPagedMaxHeads = 1024;
+constexpr long long kPagedMaxPositions = 1LL << 30;
+constexpr int kPagedMaxTokens = 1 << 22, kPagedMaxSeqs = 1 << 20;
+constexpr long long kPagedMaxRows = 1LL << 28;  // n_tokens * heads
+
+// fail(), also for calls without a context: their arguments are judged like any other's.
+template <class... Args>
+hetegen_status refuse(hetegen_ctx* ctx, hetegen_status code, const char* fmt, Args... args) {
+  return ctx ? fail(ctx, code, fmt, args...) : code;
+}
+
+// A description of a cache; nullptr when it is one, else what is wrong with it.
+const char* paged_cache(const hetegen_paged_kv* kv, hg::PagedCache* out, hetegen_status* code) {
+  *code = HETEGEN_ERR_INVALID_ARG;
+  if (!kv) return "the cache's description is NULL";
+  if (kv->heads < 1 || kv->heads > kPagedMaxHeads) return "heads outside [1, 1024]";
+  if (kv->n_pages < 1) return "n_pages below 1";
+  *code = HETEGEN_ERR_UNSUPPORTED;
+  if (kv->head_dim != 64 && kv->head_dim != 128) return "head_dim: 64 or 128";
+  if (kv->page_size != 32 && kv->page_size != 64 && kv->page_size != 128 && kv->page_size != 256)
+    return "page_size: 32, 64, 128 or 256";
+  if (kv->dtype != HETEGEN_F16 && kv->dtype != HETEGEN_BF16) return "dtype: fp16 or bf16";
+  if (kv->format != HETEGEN_KV_SAME && kv->format != HETEGEN_KV_I8 && kv->format != HETEGEN_KV_E4M3)
+    return "unknown format";
+  *out = hg::PagedCache{};
+  out->record = (long long)hg::paged_record_bytes(kv->head_dim, kv->page_size, kv->format);
+  out->heads = kv->heads;
+  out->head_dim = kv->head_dim;
+  out->page_size = kv->page_size;
+  for (int v = kv->page_size; v > 1; v >>= 1) ++out->page_shift;
+  out->n_pages = kv->n_pages;
+  out->dtype = kv->dtype;
+  out->format = kv->format;
+  *code = HETEGEN_OK;
+  return nullptr;
+}
+
+// The sizes of a batch whose rows hold `heads` heads; likewise.
+const char* paged_batch(const hetegen_paged_batch* b, const hg::PagedCache& kv, int heads, hg::PagedSeqs* out,
+                        hetegen_status* code) {
+  *code = HETEGEN_ERR_INVALID_ARG;
+  if (!b) return "the batch is NULL";
+  if (heads < 1 || heads > kPagedMaxHeads || heads % kv.heads)
+    return "query heads: a multiple of the cache's heads, at most 1024";
+  if (b->n_tokens < 0 || b->n_tokens > kPagedMaxTokens) return "n_tokens outside [0, 2^22]";
+  if ((long long)b->n_tokens * heads >= kPagedMaxRows) return "n_tokens * heads not below 2^28";
+  if (b->n_seq < 0 || b->n_seq > kPagedMaxSeqs) return "n_seq outside [0, 2^20]";
+  if (b->max_new < 1) return "max_new below 1";
+  if (b->max_pages < 1 || (long long)b->max_pages * kv.page_size > kPagedMaxPositions)
+    return "max_pages below 1, or max_pages * page_size above 2^30";
+  *out = hg::PagedSeqs{b->new_start, b->kv_len, b->page_table, b->n_tokens, b->n_seq, b->max_new, b->max_pages};
+  *code = HETEGEN_OK;
+  return nullptr;
+}
+
+bool paged_empty(const hg::PagedSeqs& b) { return b.n_tokens == 0 || b.n_seq == 0; }
+
+// The checks that every call on a cache makes; `tensors`: the call's rows, all needed unless the
+// batch is empty.
+hetegen_status paged_check(hetegen_ctx* ctx, const char* call, const hetegen_paged_kv* kv, const void* pages,
+                           const hetegen_paged_batch* b, int heads, std::initializer_list<const void*> tensors,
+                           hg::PagedCache* c, hg::PagedSeqs* s) {
+  hetegen_status code;
+  const char* what = paged_cache(kv, c, &code);
+  if (!what) what = paged_batch(b, *c, heads ? heads : c->heads, s, &code);
+  if (what) return refuse(ctx, code, "%s: %s", call, what);
+  c->pages = const_cast<void*>(pages);
+  if (paged_empty(*s)) return HETEGEN_OK;
+  if (!pages || !s->start || !s->len || !s->table)
+    return refuse(ctx, HETEGEN_ERR_INVALID_ARG, "%s: pages, new_start, kv_len and page_table are required", call);
+  if (((uintptr_t)s->start | (uintptr_t)s->len | (uintptr_t)s->table) & 3u)
+    return refuse(ctx, HETEGEN_ERR_UNSUPPORTED, "%s: new_start, kv_len and page_table must be 4-byte aligned", call);
+  for (const void* t : tensors)
+    if (!t) return refuse(ctx, HETEGEN_ERR_INVALID_ARG, "%s: a row pointer is NULL", call);
+  for (const void* t : tensors)
+    if (!aligned16(t)) return refuse(ctx, HETEGEN_ERR_UNSUPPORTED, "%s: rows must be 16-byte aligned", call);
+  if (!aligned16(pages)) return refuse(ctx, HETEGEN_ERR_UNSUPPORTED, "%s: pages must be 16-byte aligned", call);
+  return HETEGEN_OK;
+}
+
+hetegen_status paged_stride(hetegen_ctx* ctx, const char* call, long long ld, long long width) {
+  if (ld < width) return refuse(ctx, HETEGEN_ERR_INVALID_ARG, "%s: row stride %lld below %lld", call, ld, width);
+  if (ld % 8 || ld > (1LL << 40))
+    return refuse(ctx, HETEGEN_ERR_UNSUPPORTED, "%s: row stride %lld must be a multiple of 8, at most 2^40", call, ld);
+  return HETEGEN_OK;
+}
+
+hetegen_status paged_workspace(hetegen_ctx* ctx, const char* call, const void* ws, size_t have, size_t need) {
+  if (!ws || have < need)
+    return refuse(ctx, HETEGEN_ERR_INVALID_ARG, "%s: workspace of %zu bytes, %zu needed", call, ws ? have : 0, need);
+  if (!aligned16(ws)) return refuse(ctx, HETEGEN_ERR_UNSUPPORTED, "%s: the workspace must be 16-byte aligned", call);
+  return HETEGEN_OK;
+}
+
+hetegen_status paged_copy(hetegen_ctx* ctx, const char* call, const hetegen_paged_kv* kv, const void* pages,
+                          const hetegen_paged_batch* b, void* k, void* v, long long ld, hipStream_t st, bool write) {
+  if (ctx) ctx->err.clear();
+  hg::PagedCopyParams p{};
+  TRY(paged_check(ctx, call, kv, pages, b, 0, {k, v}, &p.kv, &p.seqs));
+  TRY(paged_stride(ctx, call, ld, (long long)p.kv.heads * p.kv.head_dim));
+  if (paged_empty(p.seqs)) return HETEGEN_OK;
+  if (!write && k == v) return refuse(ctx, HETEGEN_ERR_INVALID_ARG, "%s: k and v overlap", call);
+  if (!ctx) return HETEGEN_ERR_INVALID_ARG;
+  p.k = k;
+  p.v = v;
+  p.ld = ld;
+  HIPCHK(ctx, hipSetDevice(ctx->device));
+  HIPCHK(ctx, write ? hg::launch_paged_write(p, st) : hg::launch_paged_read(p, st));
+  return HETEGEN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t hetegen_paged_kv_bytes(const hetegen_paged_kv* kv) {
+  hg::PagedCache c;
+  hetegen_status code;
+  if (paged_cache(kv, &c, &code)) return 0;
+  return (size_t)c.n_pages * c.heads * c.record;
+}
+
+hetegen_status hetegen_paged_kv_write(hetegen_ctx* ctx, const hetegen_paged_kv* kv, void* pages_dev,
+                                      const hetegen_paged_batch* batch, const void* k_dev, const void* v_dev,
+                                      long long ld, void* stream) {
+  return api_guard(ctx, [&]() -> hetegen_status {
+    return paged_copy(ctx, "hetegen_paged_kv_write", kv, pages_dev, batch, const_cast<void*>(k_dev),
+                      const_cast<void*>(v_dev), ld, (hipStream_t)stream, true);
+  });
+}
+
+hetegen_status hetegen_paged_kv_read(hetegen_ctx* ctx, const hetegen_paged_kv* kv, const void* pages_dev,
+                                     const hetegen_paged_batch* batch, void* k_dev, void* v_dev, long long ld,
+                                     void* stream) {
+  return api_guard(ctx, [&]() -> hetegen_status {
+    return paged_copy(ctx, "hetegen_paged_kv_read", kv, pages_dev, batch, k_dev, v_dev, ld, (hipStream_t)stream,
+                      false);
+  });
+}
+
+size_t hetegen_paged_attention_ws_bytes(const hetegen_paged_kv* kv, const hetegen_paged_batch* batch, int heads) {
+  hg::PagedCache c;
+  hg::PagedSeqs s;
+  hetegen_status code;
+  if (paged_cache(kv, &c, &code) || paged_batch(batch, c, heads, &s, &code)) return 0;
+  return hg::paged_ws_bytes(c, s, heads);
+}
+
+hetegen_status hetegen_paged_attention(hetegen_ctx* ctx, const hetegen_paged_kv* kv, const void* pages_dev,
+                                       const hetegen_paged_batch* batch, int heads, const void* q_dev, long long ldq,
+                                       void* out_dev, long long ldo, double scale, void* ws_dev, size_t ws_bytes,
+                                       void* stream) {
+  return api_guard(ctx, [&]() -> hetegen_status {
+    if (ctx) ctx->err.clear();
+    const char* call = "hetegen_paged_attention";
+    hg::PagedAttnParams p{};
+    if (heads < 1) return refuse(ctx, HETEGEN_ERR_INVALID_ARG, "%s: heads = %d", call, heads);
+    TRY(paged_check(ctx, call, kv, pages_dev, batch, heads, {q_dev, out_dev}, &p.kv, &p.seqs));
+    TRY(paged_stride(ctx, call, ldq, (long long)heads * p.kv.head_dim));
+    TRY(paged_stride(ctx, call, ldo, (long long)heads * p.kv.head_dim));
+    if (!std::isfinite(scale)) return refuse(ctx, HETEGEN_ERR_INVALID_ARG, "%s: scale is not finite", call);
+    if (paged_empty(p.seqs)) return HETEGEN_OK;
+    if (q_dev == out_dev) return refuse(ctx, HETEGEN_ERR_INVALID_ARG, "%s: q and out overlap", call);
+    TRY(paged_workspace(ctx, call, ws_dev, ws_bytes, hg::paged_ws_bytes(p.kv, p.seqs, heads)));
+    if (!ctx) return HETEGEN_ERR_INVALID_ARG;
+    p.q = q_dev;
+    p.ldq = ldq;
+    p.out = out_dev;
+    p.ldo = ldo;
+    p.heads = heads;
+    HIPCHK(ctx, hipSetDevice(ctx->device));
+    HIPCHK(ctx, hg::launch_paged_attention(p, scale, ws_dev, (hipStream_t)stream));
+    return HETEGEN_OK;
+  });
+}
+
+size_t hetegen_decode_step_paged_ws_bytes(const hetegen_model* m, const hetegen_paged_kv* kv,
+                                          const hetegen_paged_batch* batch) {
+  if (!m || !kv || (long long)kv->heads * kv->head_dim != m->H || kv->dtype != m->dtype) return 0;
+  if (!batch || batch->n_tokens > m->max_batch) return 0;
+  const size_t a = hetegen_paged_attention_ws_bytes(kv, batch, kv->heads);
+  return a ? align256(a) + (size_t)m->max_batch * m->H * 2 : 0;
+}
+
+hetegen_status hetegen_decode_step_paged(hetegen_ctx* ctx, hetegen_model* m, const hetegen_paged_kv* kv,
+                                         void* pages_dev, const hetegen_paged_batch* batch, const void* x_dev,
+                                         void* out_dev, void* ws_dev, size_t ws_bytes, void* stream) {
+  return api_guard(ctx, [&]() -> hetegen_status {
+    if (!ctx) return HETEGEN_ERR_INVALID_ARG;
+    auto t0 = Clock::now();
+    ctx->err.clear();
+    const char* call = "hetegen_decode_step_paged";
+    if (!m) return refuse(ctx, HETEGEN_ERR_INVALID_ARG, "%s: model is NULL", call);
+    PagedStep p{};
+    TRY(paged_check(ctx, call, kv, pages_dev, batch, 0, {x_dev, out_dev}, &p.kv, &p.seqs));
+    if ((long long)kv->heads * kv->head_dim != m->H || kv->dtype != m->dtype)
+      return refuse(ctx, HETEGEN_ERR_INVALID_ARG, "%s: %d heads of %d and dtype %d do not match the model", call,
+                  kv->heads, kv->head_dim, (int)kv->dtype);
+    const int B = batch->n_tokens;
+    if (B > m->max_batch)
+      return refuse(ctx, HETEGEN_ERR_UNSUPPORTED, "%s: n_tokens = %d outside [0, %d]", call, B, m->max_batch);
+    if (paged_empty(p.seqs)) return HETEGEN_OK;
+    if (x_dev == out_dev) return refuse(ctx, HETEGEN_ERR_INVALID_ARG, "%s: x and out overlap", call);
+    if (m->trace && m->trace_bytes < hetegen_model_trace_bytes(m, B))
+      return refuse(ctx, HETEGEN_ERR_INVALID_ARG, "trace buffer too small");
+    TRY(paged_workspace(ctx, call, ws_dev, ws_bytes, hetegen_decode_step_paged_ws_bytes(m, kv, batch)));
+    p.layer_bytes = hetegen_paged_kv_bytes(kv);
+    p.ws = ws_dev;
+    p.attn = (char*)ws_dev + align256(hg::paged_ws_bytes(p.kv, p.seqs, p.kv.heads));
+    HIPCHK(ctx, hipSetDevice(ctx->device));
+    m->last_exec = HETEGEN_EXEC_EAGER;
+    hetegen_status s = enqueue_step(ctx, m, x_dev, out_dev, B, (hipStream_t)stream, -1, &p);
     if (s != HETEGEN_OK) {
       reset_pipeline(ctx);
       return s;

@@ -1,0 +1,546 @@
+// Attention of new tokens over a paged KV cache, on gfx950.
+//
+//   s_j = scale * q . K_j  for the positions j <= p that the cache holds,
+//   out = sum_j softmax(s)_j V_j      (no such position: 0)
+//
+// for every new token (position p) and query head; `group` query heads share a key/value head,
+// and the rows of a tile are (token, head of the group) pairs, so that all of them share its keys
+// and values.
+//
+// The kernel works on the matrix cores without moving the weights between lanes: keys are the
+// 16-row operand of a 16x16x32 product whose 16 columns are queries, so lane l ends up with four
+// keys' scores of query l % 16; those, rounded to 16 bits, are the 16-column operand of the product
+// with the values (whose rows are dimensions), because the order in which that product sums over
+// keys is free and the pages store the values in the order in which the scores come out.  A
+// query's running maximum and sum are the lane's own numbers.  Softmax statistics and sums are
+// binary32; scores carry log2 e.
+//
+// 8-bit caches: codes become fp16 exactly and are multiplied as fp16 (queries, too: a power of
+// two per row, taken back in the score's factor, keeps bf16 queries in range, exactly unless a value
+// is 2^29 times smaller than its row's largest).  A key's scale multiplies its score; a value's
+// scale multiplies its weight, relative to a power of two per wavefront that follows the largest
+// scale seen, so that the product stays in [0, 1].
+#include "paged_device.h"
+
+#include <math.h>
+
+#include <algorithm>
+
+namespace hg {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+template <class A, int FMT>
+struct Compute {
+  typedef F16 type;
+};
+template <class A>
+struct Compute<A, KV_SAME> {
+  typedef A type;
+};
+
+// 8 codes -> 8 fp16 values, exactly.
+template <int FMT>
+__device__ __forceinline__ u32x4 codes_f16(uint32_t lo, uint32_t hi) {
+  u32x4 r;
+  const uint32_t w[2] = {lo, hi};
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (FMT == KV_I8) {
+      // 0x6400 | u is 1024 + u; u = code + 128
+      const uint32_t u = w[h] ^ 0x80808080u;
+      const f16x2 bias = {(_Float16)1152.f, (_Float16)1152.f};
+      const f16x2 a = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - bias;
+      const f16x2 b = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - bias;
+      r[2 * h] = __builtin_bit_cast(uint32_t, a);
+      r[2 * h + 1] = __builtin_bit_cast(uint32_t, b);
+    } else {
+      r[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w[h], 1.0f, false));
+      r[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w[h], 1.0f, true));
+    }
+  }
+  return r;
+}
+
+// A query row's fragments for the key products, 8 dimensions of each 32 a lane, and *mult, what
+// turns a sum of products into a score.  ok: the row exists (0 otherwise).
+template <class A, int FMT, int D>
+__device__ __forceinline__ void load_query(const uint16_t* q, bool ok, float scale, u32x4* f, float* mult) {
+#pragma unroll
+  for (int k = 0; k < D / 32; ++k) f[k] = ok ? load16(q + 32 * k) : u32x4{0u, 0u, 0u, 0u};
+  *mult = scale;
+  if (FMT == KV_SAME && __is_same(A, F16)) return;
+  // power of two that takes the row's largest value to [2^14, 2^15) (fp16 products), or to
+  // [2^-8, 2^-7) (bf16: then no sum of products overflows whose score does not)
+  uint32_t m = 0;
+#pragma unroll
+  for (int k = 0; k < D / 32; ++k)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t w = f[k][j] & 0x7FFF7FFFu;
+      m = max(m, max(w & 0xFFFFu, w >> 16));
+    }
+  const float top = A::to_f32(groups_umax(m));
+  int e = 0;
+  if (top > 0.f && top < INFINITY) e = (FMT == KV_SAME ? -7 : 15) - __builtin_amdgcn_frexp_expf(top);
+#pragma unroll
+  for (int k = 0; k < D / 32; ++k) {
+    float v[8];
+    unpack8<A>(f[k], v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      f[k][j] = Compute<A, FMT>::type::pack(__builtin_amdgcn_ldexpf(v[2 * j], e), __builtin_amdgcn_ldexpf(v[2 * j + 1], e));
+  }
+  *mult = __builtin_amdgcn_ldexpf(scale, -e);
+}
+
+// Exponent e with v < 2^e for the largest finite of non-negative scales, as an integer that
+// compares like it (0 for none).
+__device__ __forceinline__ uint32_t finite_bits(float v) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu;
+  return b < 0x7F800000u ? b : 0u;
+}
+
+__device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// Infinities and NaNs in values.  A product gives 0 * infinity = NaN to queries that do not see a
+// key (weight 0), and to those whose weight of it rounded to 0.  The kernels look for that in
+// their sums only, at the end, and when one is not finite they walk the positions again with
+// this: it takes the infinities and NaNs out of 32 keys' values and adds them to the sums of
+// the queries that see their keys.  vis: bit e set where this lane's query sees element e of
+// this lane's group.
+template <class T, int DT>
+__device__ __forceinline__ void take_nonfinite(u32x4* vf, uint32_t vis, f32x4* O) {
+  constexpr uint32_t kOnes = 0x00010001u;                     // 1 in both halves of a word
+  constexpr uint32_t kMantissa = T::kExpLow - kOnes;
+  constexpr int kBits = __builtin_ctz(T::kExpLow);
+  const uint32_t one = T::from_f32(1.f);
+  u32x4 sees;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) sees[w] = ((vis >> (2 * w) & 1u) | (vis >> (2 * w + 1) & 1u) << 16) * one;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    u32x4 up, down, nan;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t v = vf[dt][w];
+      // an exponent of all ones carries into the sign's place
+      const uint32_t odd = ((v & T::kExp) + T::kExpLow) >> 15 & kOnes;
+      const uint32_t is_nan = odd & ((v & kMantissa) + kMantissa) >> kBits;
+      const uint32_t is_down = odd & v >> 15 & ~is_nan;
+      nan[w] = is_nan * one;
+      down[w] = is_down * one;
+      up[w] = (odd & ~is_nan & ~is_down) * one;
+      vf[dt][w] = v & ~(odd * 0xFFFFu);
+    }
+    const f32x4 u = T::mfma(up, sees, zero), d = T::mfma(down, sees, zero), n = T::mfma(nan, sees, zero);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      O[dt][i] += (u[i] > 0.f ? INFINITY : 0.f) + (d[i] > 0.f ? -INFINITY : 0.f) + (n[i] > 0.f ? NAN : 0.f);
+    __builtin_amdgcn_sched_barrier(0);  // one group of dimensions at a time: this path is rare, registers are not
+  }
+}
+
+// Partials cross workgroups on different XCDs (separate L2s): accesses that go to memory, so that
+// no cache has to be written back or emptied.
+__device__ __forceinline__ void store_through(float* p, float v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+}
+__device__ __forceinline__ float load_through(const float* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+}
+
+// ---- few rows: one token of a sequence, or some ----
+//
+// Workgroup (tile of 16 rows, key/value head, chunk of positions) of four wavefronts, each with
+// 32 positions at a time; keys and values go from memory straight into the products' operands,
+// 1 KiB a load.  The wavefronts' sums meet in LDS; a sequence of several chunks leaves partials
+// [m, l, o] in the workspace and the last workgroup of (tile, head) to arrive joins them in chunk
+// order (an arrival counter, no waiting), so results do not depend on timing.
+constexpr int kFewWaves = 4;
+constexpr int kFewShift = 4;  // rows per tile: 16
+
+template <class A, int FMT, int D>
+__global__ __launch_bounds__(64 * kFewWaves) void paged_few_kernel(PagedAttnParams p) {
+  typedef typename Compute<A, FMT>::type T;
+  constexpr int ES = FMT == KV_SAME ? 2 : 1;
+  constexpr int KK = D / 32, DT = D / 16;
+  constexpr int NL = 32 * D * ES / 1024;   // loads of 32 positions' keys (or values)
+  constexpr int OS = D + 4;
+  __shared__ __align__(16) float sacc[kFewWaves][16][OS];
+  __shared__ float sm[kFewWaves][16], sl[kFewWaves][16];
+  __shared__ int s_last;
+
+  const int head = blockIdx.x % p.kv.heads, tile = blockIdx.x / p.kv.heads;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, g = lane >> 4;
+  int local;
+  const int s = __builtin_amdgcn_readfirstlane(paged_find(p.seqs, tile, p.group, kFewShift, 1, &local));
+  if (s < 0) return;
+  const PagedSeq q = paged_load_seq(p.seqs, s, p.kv.page_shift);
+  if ((long long)q.n * p.group <= p.min_rows || (long long)q.n * p.group > p.max_rows) return;
+  const int row0 = local << kFewShift;
+  const int rows = min(q.done * p.group - row0, 16);  // of this tile
+  if (rows <= 0) return;
+  // a token at position t sees positions [0, t]; the tile's last one sees the most
+  const int last = q.first + (row0 + rows - 1) / p.group;
+  const int kend = max(min(q.held, last + 1), 0);
+  const int chunk = paged_chunk(q.held, p.splits);
+  const int nchunk = max((kend + chunk - 1) / chunk, 1);
+  const int c = blockIdx.y;
+  if (c >= nchunk) return;
+  const int j0 = c * chunk, j1 = min(j0 + chunk, kend);
+  const int nsteps = (max(j1 - j0, 0) + 31) >> 5;
+
+  const int row = row0 + col;
+  const int mypos = col < rows ? q.first + row / p.group : -1;
+  const int minpos = q.first + row0 / p.group;  // the least a row of the tile sees to
+  const int qhead = head * p.group + row % p.group;
+  u32x4 qf[KK];
+  float mult;
+  load_query<A, FMT, D>((const uint16_t*)p.q + (long long)(q.row + row / p.group) * p.ldq + qhead * D + 8 * g,
+                        col < rows, p.scale, qf, &mult);
+
+  const long long P = p.kv.page_size;
+  const int pmask = p.kv.page_size - 1;
+  const char* base = (const char*)p.kv.pages + (long long)head * p.kv.record;
+  const long long page_bytes = p.kv.record * p.kv.heads;
+
+  u32x4 kr[NL], vr[NL];
+  f32x4 ksc[2], vsc[2];
+  float m, l;
+  uint32_t seen;
+  int ve;  // values' scales are taken relative to 2^ve
+  f32x4 O[DT];
+
+  // lane i holds the page of this wavefront's step number n0 + i
+  int pages = -1;
+  auto look_up = [&](int n0) {
+    const int j = j0 + 32 * (wave + kFewWaves * (n0 + lane));
+    pages = j < j1 ? paged_page(p.seqs, p.kv, s, j) : -1;
+  };
+  auto load_keys = [&](int page, int j) {
+    const char* rec = base + max(page, 0) * page_bytes;
+    const char* src = rec + (long long)(j & pmask) * D * ES + lane * 16;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) kr[i] = load16_nt(src + i * 1024);
+    if (FMT != KV_SAME) {
+      const char* sc = rec + 2 * P * D + ((j & pmask) + 4 * g) * 4;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) ksc[t] = __builtin_bit_cast(f32x4, load16(sc + 64 * t));
+    }
+  };
+  auto load_values = [&](int page, int j) {
+    const char* rec = base + max(page, 0) * page_bytes;
+    const char* src = rec + (P + (j & pmask)) * D * ES + lane * 16;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) vr[i] = load16_nt(src + i * 1024);
+    if (FMT != KV_SAME) {
+      const char* sc = rec + 2 * P * D + P * 4 + ((j & pmask) + 4 * g) * 4;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) vsc[t] = __builtin_bit_cast(f32x4, load16(sc + 64 * t));
+    }
+  };
+
+  for (bool careful = false;; careful = true) {
+    m = -INFINITY;
+    l = 0.f;
+    seen = 0;
+    ve = -126;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) O[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    int page = -1, n = 0;
+    if (wave < nsteps) {
+      look_up(0);
+      page = __builtin_amdgcn_readlane(pages, 0);
+      load_keys(page, j0 + 32 * wave);
+      load_values(page, j0 + 32 * wave);
+    }
+    for (int st = wave; st < nsteps; st += kFewWaves) {
+      const int jb = j0 + 32 * st;
+      const bool more = st + kFewWaves < nsteps;
+      int next = -1;
+      if (more) {
+        if ((++n & 63) == 0) look_up(n);
+        next = __builtin_amdgcn_readlane(pages, n & 63);
+      }
+      // scores
+      f32x4 sc[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KK; ++k) {
+          u32x4 kf;
+          if (FMT == KV_SAME) {
+            kf = kr[t * KK + k];
+          } else {
+            const u32x4& w = kr[t * (KK / 2) + (k >> 1)];
+            kf = codes_f16<FMT>(w[2 * (k & 1)], w[2 * (k & 1) + 1]);
+          }
+          acc = T::mfma(kf, qf[k], acc);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[t][i] = FMT == KV_SAME ? acc[i] * mult : acc[i] * (mult * ksc[t][i]);
+      }
+      if (more) load_keys(next, jb + 32 * kFewWaves);
+      // the last positions, and positions of a page that is not there, are masked
+      const bool whole = page >= 0 && jb + 32 <= q.held;
+      const bool full = whole && jb + 31 <= minpos;
+      uint32_t vis = 0xFFu;
+      if (!full) {
+        vis = 0u;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int j = jb + 16 * (e >> 2) + 4 * g + (e & 3);
+          const bool see = page >= 0 && j < q.held && j <= mypos;
+          vis |= (uint32_t)see << e;
+          if (!see) sc[e >> 2][e & 3] = -INFINITY;
+        }
+      }
+      seen |= vis;
+      float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
+                       fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+      mx = fmaxf(m, groups_max(mx));
+      const float ms = mx == -INFINITY ? 0.f : mx;
+      float al = exp2_hw(m - ms);
+      m = mx;
+      float w[8], sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        w[e] = exp2_hw(sc[e >> 2][e & 3] - ms);
+        sum += w[e];
+      }
+      l = fmaf(l, al, sum);
+      if (FMT != KV_SAME) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int j = jb + 16 * (e >> 2) + 4 * g + (e & 3);
+          top = max(top, whole || (page >= 0 && j < q.held) ? finite_bits(vsc[e >> 2][e & 3]) : 0u);
+        }
+        const int e2 = max(ve, (int)(groups_umax(top) >> 23) - 126);
+        al = __builtin_amdgcn_ldexpf(al, ve - e2);
+        ve = e2;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float r = w[e] * __builtin_amdgcn_ldexpf(vsc[e >> 2][e & 3], -ve);
+          w[e] = (vis >> e) & 1 ? r : 0.f;
+        }
+      }
+      if (__ballot(al != 1.f)) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) O[dt][i] *= al;
+      }
+      // weights to 16 bits twice: a second product takes what the first rounding left (memory is
+      // what bounds this kernel), so that weights count as in binary32 but for fp16's smallest step
+      u32x4 pf, pl;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        pf[i] = T::pack(w[2 * i], w[2 * i + 1]);
+        pl[i] = T::pack(w[2 * i] - T::to_f32(pf[i] & 0xFFFFu), w[2 * i + 1] - T::to_f32(pf[i] >> 16));
+      }
+      u32x4 vf[DT];
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        if (FMT == KV_SAME) vf[dt] = vr[dt];
+        else vf[dt] = codes_f16<FMT>(vr[dt >> 1][2 * (dt & 1)], vr[dt >> 1][2 * (dt & 1) + 1]);
+      }
+      if (!whole) {
+        // what lies behind a sequence's end was never written: it may be anything
+        u32x4 keep;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = jb + 16 * (i >> 1) + 4 * g + 2 * (i & 1);
+          keep[i] = page < 0 ? 0u : (j < q.held ? 0xFFFFu : 0u) | (j + 1 < q.held ? 0xFFFF0000u : 0u);
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vf[dt] &= keep;
+      }
+      if (FMT == KV_SAME && careful) take_nonfinite<T, DT>(vf, vis, O);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        O[dt] = T::mfma(vf[dt], pf, O[dt]);
+        O[dt] = T::mfma(vf[dt], pl, O[dt]);
+      }
+      if (more) load_values(next, jb + 32 * kFewWaves);
+      page = next;
+    }
+    if (FMT != KV_SAME || careful) break;
+    bool odd = false;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) odd |= !(fabsf(O[dt][i]) < INFINITY);
+    if (!__ballot(odd)) break;
+  }
+
+  // a row that saw positions, all of score -infinity, has no softmax: NaN, as the formula has it
+  l = groups_sum(l);
+  if (m == -INFINITY && groups_umax(seen) != 0) l = NAN;
+  if (col < rows) {
+    if (g == 0) {
+      sm[wave][col] = m;
+      sl[wave][col] = l;
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      f32x4 o = O[dt];
+      if (FMT != KV_SAME) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_ldexpf(o[i], ve);
+      }
+      *(f32x4*)&sacc[wave][col][16 * dt + 4 * g] = o;
+    }
+  }
+  __syncthreads();
+
+  // the wavefronts' sums, in order; one without a visible position has m = -inf and weight 0
+  auto joined = [&](int r, int d, float* M, float* L) {
+    float mx = sm[0][r];
+#pragma unroll
+    for (int i = 1; i < kFewWaves; ++i) mx = fmaxf(mx, sm[i][r]);
+    float o = 0.f, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kFewWaves; ++i) {
+      if (sm[i][r] == -INFINITY) {
+        if (mx == -INFINITY) sum += sl[i][r];
+      } else {
+        const float f = exp2_hw(sm[i][r] - mx);
+        o = fmaf(f, sacc[i][r][d], o);
+        sum = fmaf(f, sl[i][r], sum);
+      }
+    }
+    *M = mx;
+    *L = sum;
+    return o;
+  };
+  auto out_at = [&](int r) {
+    const int rr = row0 + r;
+    return (uint16_t*)p.out + (long long)(q.row + rr / p.group) * p.ldo + (head * p.group + rr % p.group) * D;
+  };
+  auto part_at = [&](int r) {
+    const int rr = row0 + r;
+    return p.part + ((long long)(q.row + rr / p.group) * p.heads + head * p.group + rr % p.group) * p.splits * (D + 2);
+  };
+  if (nchunk == 1) {
+    for (int i = threadIdx.x; i < rows * D; i += 64 * kFewWaves) {
+      float M, L;
+      const float o = joined(i / D, i % D, &M, &L);
+      out_at(i / D)[i % D] = A::from_f32(L == 0.f ? 0.f : o / L);
+    }
+    return;
+  }
+  for (int i = threadIdx.x; i < rows * D; i += 64 * kFewWaves) {
+    const int r = i / D, d = i % D;
+    float M, L;
+    const float o = joined(r, d, &M, &L);
+    float* at = part_at(r) + (long long)c * (D + 2);
+    store_through(at + 2 + d, o);
+    if (d == 0) {
+      store_through(at, M);
+      store_through(at + 1, L);
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0);  // this thread's partials are in memory
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    uint32_t* cnt = p.cnt + blockIdx.x;
+    const uint32_t prev = __hip_atomic_fetch_add(cnt, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    s_last = prev == (uint32_t)(nchunk - 1);
+    if (s_last) __hip_atomic_store(cnt, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (!s_last) return;
+  // join the chunks, in order; weights of a row's chunks in LDS
+  float* weight = &sacc[0][0][0];  // [16][kPagedMaxSplits]
+  static_assert(16 * kPagedMaxSplits <= kFewWaves * 16 * OS, "chunk weights");
+  for (int i = threadIdx.x; i < rows * nchunk; i += 64 * kFewWaves) {
+    const int r = i / nchunk, k = i % nchunk;
+    weight[r * kPagedMaxSplits + k] = load_through(part_at(r) + (long long)k * (D + 2));
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * D; i += 64 * kFewWaves) {
+    const int r = i / D, d = i % D;
+    const float* at = part_at(r);
+    float M = -INFINITY, L = 0.f, o = 0.f;
+    for (int k = 0; k < nchunk; ++k) M = fmaxf(M, weight[r * kPagedMaxSplits + k]);
+    for (int k0 = 0; k0 < nchunk; k0 += 8) {
+      float ov[8], lv[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float* a = at + (long long)min(k0 + u, nchunk - 1) * (D + 2);
+        ov[u] = load_through(a + 2 + d);
+        lv[u] = load_through(a + 1);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        if (k0 + u >= nchunk) continue;
+        const float mk = weight[r * kPagedMaxSplits + k0 + u];
+        if (mk == -INFINITY) {
+          if (M == -INFINITY) L += lv[u];
+        } else {
+          const float f = exp2_hw(mk - M);
+          L = fmaf(f, lv[u], L);
+          o = fmaf(f, ov[u], o);
+        }
+      }
+    }
+    out_at(r)[d] = A::from_f32(L == 0.f ? 0.f : o / L);
+  }
+}
+
+template <class A, int FMT, int D>
+hipError_t few_t(const PagedAttnParams& p, const dim3& grid, hipStream_t st) {
+  hipLaunchKernelGGL((paged_few_kernel<A, FMT, D>), grid, dim3(64 * kFewWaves), 0, st, p);
+  return hipGetLastError();
+}
+
+template <class A>
+hipError_t few_a(const PagedAttnParams& p, const dim3& grid, hipStream_t st) {
+  const bool wide = p.kv.head_dim == 128;
+  switch (p.kv.format) {
+    case KV_SAME: return wide ? few_t<A, KV_SAME, 128>(p, grid, st) : few_t<A, KV_SAME, 64>(p, grid, st);
+    case KV_I8: return wide ? few_t<A, KV_I8, 128>(p, grid, st) : few_t<A, KV_I8, 64>(p, grid, st);
+  }
+  return wide ? few_t<A, KV_E4M3, 128>(p, grid, st) : few_t<A, KV_E4M3, 64>(p, grid, st);
+}
+
+// Splits of a sequence that the partials have room for: kMaxPartials rows of all chunks.
+constexpr long long kMaxPartials = 1 << 18;
+int few_splits(const PagedCache& kv, const PagedSeqs& b, int heads) {
+  const long long rows = (long long)b.n_tokens * heads;
+  if (rows * 2 > kMaxPartials || paged_tiles(b, heads / kv.heads, kFewShift, 1) * kv.heads > kPagedCounters) return 1;
+  return (int)std::min<long long>(kPagedMaxSplits, kMaxPartials / rows);
+}
+
+}  // namespace
+
+size_t paged_ws_bytes(const PagedCache& kv, const PagedSeqs& b, int heads) {
+  const long long cap = (long long)b.max_pages << kv.page_shift;
+  const long long chunks = std::min<long long>((cap + 127) / 128, kPagedMaxSplits);
+  const long long rows = (long long)b.n_tokens * heads;
+  const long long few = std::min(rows * chunks, kMaxPartials);
+  return kPagedCounters * sizeof(uint32_t) + (size_t)few * (kv.head_dim + 2) * sizeof(float);
+}
+
+hipError_t launch_paged_attention(PagedAttnParams p, double scale, void* ws, hipStream_t stream) {
+  if (p.seqs.n_tokens < 1 || p.seqs.n_seq < 1) return hipSuccess;
+  p.group = p.heads / p.kv.heads;
+  p.scale = (float)(scale * (double)kLog2e);
+  p.cnt = (uint32_t*)ws;
+  p.part = (float*)(p.cnt + kPagedCounters);
+  const long long cap = (long long)p.seqs.max_pages << p.kv.page_shift;
+  p.splits = few_splits(p.kv, p.seqs, p.heads);
+  p.splits = (int)std::min<long long>(p.splits, (cap + 127) / 128);
+  p.min_rows = 0;
+  p.max_rows = 0x7FFFFFFF;
+  const dim3 grid((unsigned)(paged_tiles(p.seqs, p.group, kFewShift, 1) * p.kv.heads), (unsigned)p.splits);
+  return p.kv.dtype == 1 ? few_a<BF16>(p, grid, stream) : few_a<F16>(p, grid, stream);
+}
+
+}  // namespace hg
