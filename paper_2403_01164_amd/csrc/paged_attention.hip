@@ -7,7 +7,7 @@
 // and the rows of a tile are (token, head of the group) pairs, so that all of them share its keys
 // and values.
 //
-// The kernel works on the matrix cores without moving the weights between lanes: keys are the
+// Both kernels work on the matrix cores without moving the weights between lanes: keys are the
 // 16-row operand of a 16x16x32 product whose 16 columns are queries, so lane l ends up with four
 // keys' scores of query l % 16; those, rounded to 16 bits, are the 16-column operand of the product
 // with the values (whose rows are dimensions), because the order in which that product sums over
@@ -30,6 +30,7 @@ namespace hg {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kTiny = 1.4e-45f;  // the least factor of a score: with 0, a masked one would be -inf * 0
 
 template <class A, int FMT>
 struct Compute {
@@ -64,12 +65,16 @@ __device__ __forceinline__ u32x4 codes_f16(uint32_t lo, uint32_t hi) {
 }
 
 // A query row's fragments for the key products, 8 dimensions of each 32 a lane, and *mult, what
-// turns a sum of products into a score.  ok: the row exists (0 otherwise).
+// turns a sum of products into a score (positive: a negative scale changes the query's sign).  ok: the row exists (0 otherwise).
 template <class A, int FMT, int D>
 __device__ __forceinline__ void load_query(const uint16_t* q, bool ok, float scale, u32x4* f, float* mult) {
 #pragma unroll
-  for (int k = 0; k < D / 32; ++k) f[k] = ok ? load16(q + 32 * k) : u32x4{0u, 0u, 0u, 0u};
-  *mult = scale;
+  for (int k = 0; k < D / 32; ++k) {
+    f[k] = ok ? load16(q + 32 * k) : u32x4{0u, 0u, 0u, 0u};
+    f[k] ^= scale < 0.f ? 0x80008000u : 0u;
+  }
+  scale = fabsf(scale);
+  *mult = fmaxf(scale, kTiny);
   if (FMT == KV_SAME && __is_same(A, F16)) return;
   // power of two that takes the row's largest value to [2^14, 2^15) (fp16 products), or to
   // [2^-8, 2^-7) (bf16: then no sum of products overflows whose score does not)
@@ -92,7 +97,7 @@ __device__ __forceinline__ void load_query(const uint16_t* q, bool ok, float sca
     for (int j = 0; j < 4; ++j)
       f[k][j] = Compute<A, FMT>::type::pack(__builtin_amdgcn_ldexpf(v[2 * j], e), __builtin_amdgcn_ldexpf(v[2 * j + 1], e));
   }
-  *mult = __builtin_amdgcn_ldexpf(scale, -e);
+  *mult = fmaxf(__builtin_amdgcn_ldexpf(scale, -e), kTiny);
 }
 
 // Exponent e with v < 2^e for the largest finite of non-negative scales, as an integer that
@@ -110,37 +115,41 @@ __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2
 // this: it takes the infinities and NaNs out of 32 keys' values and adds them to the sums of
 // the queries that see their keys.  vis: bit e set where this lane's query sees element e of
 // this lane's group.
-template <class T, int DT>
-__device__ __forceinline__ void take_nonfinite(u32x4* vf, uint32_t vis, f32x4* O) {
-  constexpr uint32_t kOnes = 0x00010001u;                     // 1 in both halves of a word
+template <class T>
+__device__ __forceinline__ u32x4 seen_keys(uint32_t vis) {
+  u32x4 r;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) r[w] = ((vis >> (2 * w) & 1u) | (vis >> (2 * w + 1) & 1u) << 16) * (uint32_t)T::from_f32(1.f);
+  return r;
+}
+// v: 16 dimensions of 32 keys; sees[u] = seen_keys of the u-th 16 queries, *O[u] their sums.
+template <class T, int U>
+__device__ __forceinline__ void take_nonfinite(u32x4& v, const u32x4* sees, f32x4* const* O) {
+  constexpr uint32_t kOnes = 0x00010001u;  // 1 in both halves of a word
   constexpr uint32_t kMantissa = T::kExpLow - kOnes;
   constexpr int kBits = __builtin_ctz(T::kExpLow);
   const uint32_t one = T::from_f32(1.f);
-  u32x4 sees;
+  u32x4 up, down, nan;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) sees[w] = ((vis >> (2 * w) & 1u) | (vis >> (2 * w + 1) & 1u) << 16) * one;
+  for (int w = 0; w < 4; ++w) {
+    // an exponent of all ones carries into the sign's place
+    const uint32_t odd = ((v[w] & T::kExp) + T::kExpLow) >> 15 & kOnes;
+    const uint32_t is_nan = odd & ((v[w] & kMantissa) + kMantissa) >> kBits;
+    const uint32_t is_down = odd & v[w] >> 15 & ~is_nan;
+    nan[w] = is_nan * one;
+    down[w] = is_down * one;
+    up[w] = (odd & ~is_nan & ~is_down) * one;
+    v[w] &= ~(odd * 0xFFFFu);
+  }
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) {
-    u32x4 up, down, nan;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const uint32_t v = vf[dt][w];
-      // an exponent of all ones carries into the sign's place
-      const uint32_t odd = ((v & T::kExp) + T::kExpLow) >> 15 & kOnes;
-      const uint32_t is_nan = odd & ((v & kMantissa) + kMantissa) >> kBits;
-      const uint32_t is_down = odd & v >> 15 & ~is_nan;
-      nan[w] = is_nan * one;
-      down[w] = is_down * one;
-      up[w] = (odd & ~is_nan & ~is_down) * one;
-      vf[dt][w] = v & ~(odd * 0xFFFFu);
-    }
-    const f32x4 u = T::mfma(up, sees, zero), d = T::mfma(down, sees, zero), n = T::mfma(nan, sees, zero);
+  for (int u = 0; u < U; ++u) {
+    const f32x4 a = T::mfma(up, sees[u], zero), b = T::mfma(down, sees[u], zero), c = T::mfma(nan, sees[u], zero);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      O[dt][i] += (u[i] > 0.f ? INFINITY : 0.f) + (d[i] > 0.f ? -INFINITY : 0.f) + (n[i] > 0.f ? NAN : 0.f);
-    __builtin_amdgcn_sched_barrier(0);  // one group of dimensions at a time: this path is rare, registers are not
+      (*O[u])[i] += (a[i] > 0.f ? INFINITY : 0.f) + (b[i] > 0.f ? -INFINITY : 0.f) + (c[i] > 0.f ? NAN : 0.f);
   }
+  __builtin_amdgcn_sched_barrier(0);  // one fragment at a time: this path is rare, registers are not
 }
 
 // Partials cross workgroups on different XCDs (separate L2s): accesses that go to memory, so that
@@ -163,7 +172,7 @@ constexpr int kFewWaves = 4;
 constexpr int kFewShift = 4;  // rows per tile: 16
 
 template <class A, int FMT, int D>
-__global__ __launch_bounds__(64 * kFewWaves) void paged_few_kernel(PagedAttnParams p) {
+__global__ __launch_bounds__(64 * kFewWaves, 2) void paged_few_kernel(PagedAttnParams p) {
   typedef typename Compute<A, FMT>::type T;
   constexpr int ES = FMT == KV_SAME ? 2 : 1;
   constexpr int KK = D / 32, DT = D / 16;
@@ -289,15 +298,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few_kernel(PagedAttnPara
       // the last positions, and positions of a page that is not there, are masked
       const bool whole = page >= 0 && jb + 32 <= q.held;
       const bool full = whole && jb + 31 <= minpos;
+      const int top = (page >= 0 ? q.held - 1 : -1) - (jb + 4 * g);  // element e is held if up to here
       uint32_t vis = 0xFFu;
       if (!full) {
+        const int to = min(mypos - (jb + 4 * g), top);
         vis = 0u;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int j = jb + 16 * (e >> 2) + 4 * g + (e & 3);
-          const bool see = page >= 0 && j < q.held && j <= mypos;
-          vis |= (uint32_t)see << e;
-          if (!see) sc[e >> 2][e & 3] = -INFINITY;
+          const bool see = 16 * (e >> 2) + (e & 3) <= to;
+          vis |= (see ? 1u : 0u) << e;
+          sc[e >> 2][e & 3] = see ? sc[e >> 2][e & 3] : -INFINITY;
         }
       }
       seen |= vis;
@@ -315,13 +325,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few_kernel(PagedAttnPara
       }
       l = fmaf(l, al, sum);
       if (FMT != KV_SAME) {
-        uint32_t top = 0;
+        uint32_t most = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int j = jb + 16 * (e >> 2) + 4 * g + (e & 3);
-          top = max(top, whole || (page >= 0 && j < q.held) ? finite_bits(vsc[e >> 2][e & 3]) : 0u);
-        }
-        const int e2 = max(ve, (int)(groups_umax(top) >> 23) - 126);
+        for (int e = 0; e < 8; ++e)
+          most = max(most, 16 * (e >> 2) + (e & 3) <= top ? finite_bits(vsc[e >> 2][e & 3]) : 0u);
+        const int e2 = max(ve, (int)(groups_umax(most) >> 23) - 126);
         al = __builtin_amdgcn_ldexpf(al, ve - e2);
         ve = e2;
 #pragma unroll
@@ -355,13 +363,20 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few_kernel(PagedAttnPara
         u32x4 keep;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int j = jb + 16 * (i >> 1) + 4 * g + 2 * (i & 1);
-          keep[i] = page < 0 ? 0u : (j < q.held ? 0xFFFFu : 0u) | (j + 1 < q.held ? 0xFFFF0000u : 0u);
+          const int to = top - (16 * (i >> 1) + 2 * (i & 1));
+          keep[i] = (to >= 0 ? 0xFFFFu : 0u) | (to >= 1 ? 0xFFFF0000u : 0u);
         }
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) vf[dt] &= keep;
       }
-      if (FMT == KV_SAME && careful) take_nonfinite<T, DT>(vf, vis, O);
+      if (FMT == KV_SAME && careful) {
+        const u32x4 sees = seen_keys<T>(vis);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          f32x4* const o[1] = {&O[dt]};
+          take_nonfinite<T, 1>(vf[dt], &sees, o);
+        }
+      }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         O[dt] = T::mfma(vf[dt], pf, O[dt]);
@@ -494,6 +509,401 @@ __global__ __launch_bounds__(64 * kFewWaves) void paged_few_kernel(PagedAttnPara
   }
 }
 
+// ---- many rows: prompts and chunks of them ----
+//
+// Workgroup (tile of 128 rows, key/value head, share of the positions) of four wavefronts of 32
+// rows each; 64 positions at a time go through LDS, one buffer being filled while the other is
+// multiplied: 16-bit pages by loads that write to LDS themselves (the pages' order is the operands'
+// order already), 8-bit ones through registers, where they become fp16.  Every operand read from
+// LDS feeds two products.  When there are few tiles, several workgroups share a tile's positions
+// and a second kernel joins their partials.
+constexpr int kManyWaves = 4;
+constexpr int kManyShift = 7;  // rows per tile: 128
+constexpr int kManyKeys = 64;  // positions at a time
+constexpr int kManyMaxSplits = 16;
+constexpr int kManyWorkgroups = 512;  // two for each of the 256 CUs
+
+// Shares of a tile's positions [0, kend): `per` steps of kManyKeys each, *used of them.
+__device__ __forceinline__ int many_share(int kend, int splits, int* used) {
+  const int steps = (kend + kManyKeys - 1) / kManyKeys;
+  const int per = max((steps + splits - 1) / splits, 1);
+  *used = max((steps + per - 1) / per, 1);
+  return per;
+}
+
+template <class A, int FMT, int D>
+__global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAttnParams p) {
+  typedef typename Compute<A, FMT>::type T;
+  constexpr int ES = FMT == KV_SAME ? 2 : 1;
+  constexpr int KK = D / 32, DT = D / 16, U = 2;
+  constexpr int KT = kManyKeys / 16;             // key tiles of a step
+  constexpr int kSide = kManyKeys * D * 2;       // bytes of a step's keys (or values) in LDS
+  constexpr int NL = kManyKeys * D * ES * 2 / 1024 / kManyWaves;  // loads of a step, per wavefront
+  __shared__ __align__(16) char buf0[2 * kSide], buf1[2 * kSide];
+  __shared__ float scales[2][FMT == KV_SAME ? 1 : 2 * kManyKeys];
+  __shared__ int s_odd;
+
+  const int head = blockIdx.x % p.kv.heads, tile = blockIdx.x / p.kv.heads;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, g = lane >> 4;
+  int local;
+  const int s = __builtin_amdgcn_readfirstlane(paged_find(p.seqs, tile, p.group, kManyShift, 1, &local));
+  if (s < 0) return;
+  const PagedSeq q = paged_load_seq(p.seqs, s, p.kv.page_shift);
+  if ((long long)q.n * p.group <= p.min_rows) return;
+  const int all = q.done * p.group;
+  local = ((all + (1 << kManyShift) - 1) >> kManyShift) - 1 - local;  // the rows that see most come first
+  if (local < 0) return;
+  const int row0 = local << kManyShift;
+  const int rows = min(all - row0, 1 << kManyShift);
+  const int kend = max(min(q.held, q.first + (row0 + rows - 1) / p.group + 1), 0);
+  int used;
+  const int per = many_share(kend, p.splits, &used);
+  const int c = blockIdx.y;
+  if (c >= used) return;
+  const int j0 = c * per * kManyKeys, j1 = min(j0 + per * kManyKeys, kend);
+  const int nsteps = (max(j1 - j0, 0) + kManyKeys - 1) / kManyKeys;
+
+  // this wavefront's rows
+  const int wrow = row0 + 32 * wave, wrows = min(rows - 32 * wave, 32);
+  const int wmin = q.first + wrow / p.group;                                       // its first row sees to here,
+  const int wmax = wrows > 0 ? q.first + (wrow + wrows - 1) / p.group : -1;        // its last one to here
+  u32x4 qf[U][KK];
+  float mult[U];
+  int mypos[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int row = wrow + 16 * u + col;
+    const bool ok = 16 * u + col < wrows;
+    mypos[u] = ok ? q.first + row / p.group : -1;
+    load_query<A, FMT, D>((const uint16_t*)p.q + (long long)(q.row + row / p.group) * p.ldq +
+                              (head * p.group + row % p.group) * D + 8 * g,
+                          ok, p.scale, qf[u], &mult[u]);
+  }
+
+  const long long P = p.kv.page_size;
+  const int pmask = p.kv.page_size - 1;
+  const char* base = (const char*)p.kv.pages + (long long)head * p.kv.record;
+  const long long page_bytes = p.kv.record * p.kv.heads;
+
+  f32x4 O[U][DT];
+  float m[U], l[U];
+  uint32_t seen[U];
+  int ve;
+  int pages = -1;  // lane i: the page of the i-th 32 positions from the last look-up on
+  u32x4 raw[NL];   // 8-bit pages on their way to LDS
+  float raw_scale = 0.f;
+
+  // a step's 32-position halves: their pages (-1: none)
+  auto half_pages = [&](int step, int* a, int* b) {
+    const int i = 2 * (step & 31);
+    if (i == 0) {
+      const int j = j0 + kManyKeys * step + 32 * lane;
+      pages = j < j1 ? paged_page(p.seqs, p.kv, s, j) : -1;
+    }
+    *a = __builtin_amdgcn_readlane(pages, i);
+    *b = __builtin_amdgcn_readlane(pages, i + 1);
+  };
+  auto issue = [&](char* buf, int step, int pa, int pb) {
+    const int half = wave & 1, side = wave >> 1;  // a wavefront brings one half's keys or values
+    const int j = j0 + kManyKeys * step + 32 * half;
+    const char* rec = base + max(half ? pb : pa, 0) * page_bytes;
+    const char* src = rec + (side * P + (j & pmask)) * D * ES + lane * 16;
+    if (FMT == KV_SAME) {
+      char* dst = buf + side * kSide + half * (kSide / 2);
+#pragma unroll
+      for (int i = 0; i < NL; ++i)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + i * 1024),
+                                         (__attribute__((address_space(3))) void*)(dst + i * 1024), 16, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) raw[i] = load16(src + i * 1024);
+      if (lane < 32) raw_scale = ((const float*)(rec + 2 * P * D))[side * P + (j & pmask) + lane];
+    }
+  };
+  auto commit = [&](char* buf, int b) {
+    if (FMT != KV_SAME) {
+      const int half = wave & 1, side = wave >> 1;
+      char* dst = buf + side * kSide + half * (kSide / 2) + lane * 16;
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        *(u32x4*)(dst + 2 * i * 1024) = codes_f16<FMT>(raw[i][0], raw[i][1]);
+        *(u32x4*)(dst + (2 * i + 1) * 1024) = codes_f16<FMT>(raw[i][2], raw[i][3]);
+      }
+      if (lane < 32) scales[b][side * kManyKeys + 32 * half + lane] = raw_scale;
+    }
+  };
+  auto compute = [&](const char* buf, int b, int step, int pa, int pb, bool careful) {
+    const int jb = j0 + kManyKeys * step;
+    if (jb > wmax) return;
+    const char* kb = buf + lane * 16;
+    const char* vb = buf + kSide + lane * 16;
+    f32x4 sc[KT][U];
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) sc[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KK; ++k) {
+        const u32x4 kf = *(const u32x4*)(kb + (t * KK + k) * 1024);
+#pragma unroll
+        for (int u = 0; u < U; ++u) sc[t][u] = T::mfma(kf, qf[u][k], sc[t][u]);
+      }
+      if (FMT != KV_SAME) {
+        const f32x4 ks = *(const f32x4*)&scales[b][16 * t + 4 * g];
+#pragma unroll
+        for (int u = 0; u < U; ++u) sc[t][u] *= ks;
+      }
+    }
+    const bool whole = pa >= 0 && pb >= 0 && jb + kManyKeys <= q.held;
+    const bool full = whole && jb + kManyKeys - 1 <= wmin;
+    // last position of either half that is in the cache
+    const int top[2] = {pa >= 0 ? q.held - 1 : -1, pb >= 0 ? q.held - 1 : -1};
+    const int jl = jb + 4 * g;  // element i of key tile t is position jl + 16 t + i
+    uint32_t vis[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      vis[u] = 0xFFFFu;
+      if (!full) {
+        vis[u] = 0u;
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+          const int to = min(mypos[u], top[t >> 1]) - (jl + 16 * t);  // elements up to here are seen
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            vis[u] |= (i <= to ? 1u : 0u) << (4 * t + i);
+            sc[t][u][i] = i <= to ? sc[t][u][i] : -INFINITY;
+          }
+        }
+      }
+      seen[u] |= vis[u];
+    }
+    // values' scales, relative to the largest so far
+    f32x4 vs[KT];
+    int e2 = ve;
+    if (FMT != KV_SAME) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+        vs[t] = *(const f32x4*)&scales[b][kManyKeys + 16 * t + 4 * g];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = max(most, i <= top[t >> 1] - (jl + 16 * t) ? finite_bits(vs[t][i]) : 0u);
+      }
+      e2 = max(ve, (int)(groups_umax(most) >> 23) - 126);
+      const float to = __builtin_amdgcn_ldexpf(1.f, -e2);
+#pragma unroll
+      for (int t = 0; t < KT; ++t) vs[t] *= to;
+    }
+    u32x4 pf[U][KT / 2];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+        mx = fmaxf(mx, fmaxf(fmaxf(sc[t][u][0], sc[t][u][1]), fmaxf(sc[t][u][2], sc[t][u][3])));
+      mx = fmaxf(m[u], groups_max(mx) * mult[u]);
+      const float ms = mx == -INFINITY ? 0.f : mx;
+      float al = exp2_hw(m[u] - ms), sum = 0.f;
+      m[u] = mx;
+      float w[KT * 4];
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          w[4 * t + i] = exp2_hw(fmaf(sc[t][u][i], mult[u], -ms));
+          sum += w[4 * t + i];
+        }
+      l[u] = fmaf(l[u], al, sum);
+      if (FMT != KV_SAME) {
+        al = __builtin_amdgcn_ldexpf(al, ve - e2);
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            w[4 * t + i] = vis[u] >> (4 * t + i) & 1u ? w[4 * t + i] * vs[t][i] : 0.f;
+      }
+      if (__ballot(al != 1.f)) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) O[u][dt] *= al;
+      }
+      // weights rounded to 16 bits once: their errors average out over the positions
+#pragma unroll
+      for (int h = 0; h < KT / 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pf[u][h][i] = T::pack(w[8 * h + 2 * i], w[8 * h + 2 * i + 1]);
+    }
+    ve = e2;
+    if (whole && !careful) {
+#pragma unroll
+      for (int h = 0; h < KT / 2; ++h)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const u32x4 vf = *(const u32x4*)(vb + h * (kSide / 2) + dt * 1024);
+#pragma unroll
+          for (int u = 0; u < U; ++u) O[u][dt] = T::mfma(vf, pf[u][h], O[u][dt]);
+        }
+      return;
+    }
+    // what lies behind a sequence's end was never written: it may be anything
+#pragma unroll
+    for (int h = 0; h < KT / 2; ++h) {
+      u32x4 keep, sees[U];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int to = top[h] - (jl + 32 * h + 16 * (i >> 1) + 2 * (i & 1));
+        keep[i] = (to >= 0 ? 0xFFFFu : 0u) | (to >= 1 ? 0xFFFF0000u : 0u);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) sees[u] = seen_keys<T>(vis[u] >> (8 * h));
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        u32x4 vf = *(const u32x4*)(vb + h * (kSide / 2) + dt * 1024) & keep;
+        if (FMT == KV_SAME && careful) {
+          f32x4* const o[2] = {&O[0][dt], &O[1][dt]};
+          take_nonfinite<T, U>(vf, sees, o);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) O[u][dt] = T::mfma(vf, pf[u][h], O[u][dt]);
+      }
+    }
+  };
+
+  for (bool careful = false;; careful = true) {
+    ve = -126;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      m[u] = -INFINITY;
+      l[u] = 0.f;
+      seen[u] = 0;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) O[u][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    int pa = -1, pb = -1;
+    if (nsteps > 0) {
+      half_pages(0, &pa, &pb);
+      issue(buf0, 0, pa, pb);
+      commit(buf0, 0);
+    }
+    // one barrier a step: behind it the step's buffer is filled and nobody reads the other one
+    auto turn = [&](char* now, char* other, int b, int step) {
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      int na = -1, nb = -1;
+      const bool more = step + 1 < nsteps;
+      if (more) {
+        half_pages(step + 1, &na, &nb);
+        issue(other, step + 1, na, nb);
+      }
+      compute(now, b, step, pa, pb, careful);
+      if (more) commit(other, 1 - b);
+      pa = na;
+      pb = nb;
+    };
+    for (int step = 0; step < nsteps; step += 2) {
+      turn(buf0, buf1, 0, step);
+      if (step + 1 < nsteps) turn(buf1, buf0, 1, step + 1);
+    }
+    if (FMT != KV_SAME || careful) break;
+    bool odd = false;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) odd |= !(fabsf(O[u][dt][i]) < INFINITY);
+    // the wavefronts share the buffers, so they walk again together
+    if (threadIdx.x == 0) s_odd = 0;
+    __syncthreads();
+    if (__ballot(odd) && lane == 0) s_odd = 1;
+    __syncthreads();
+    if (!s_odd) break;
+  }
+
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    l[u] = groups_sum(l[u]);
+    if (m[u] == -INFINITY && groups_umax(seen[u]) != 0) l[u] = NAN;
+    const int row = wrow + 16 * u + col;
+    if (16 * u + col >= wrows) continue;
+    const long long token = q.row + row / p.group;
+    const int qhead = head * p.group + row % p.group;
+    if (used == 1) {
+      const float r = l[u] == 0.f ? 0.f : 1.f / l[u];
+      uint16_t* out = (uint16_t*)p.out + token * p.ldo + qhead * D + 4 * g;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        f32x4 o = O[u][dt];
+        if (FMT != KV_SAME) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_ldexpf(o[i], ve);
+        }
+        if (l[u] == 0.f) o = f32x4{0.f, 0.f, 0.f, 0.f};
+        *(u32x2*)(out + 16 * dt) = u32x2{A::pack(o[0] * r, o[1] * r), A::pack(o[2] * r, o[3] * r)};
+      }
+    } else {
+      const long long at = (token * p.heads + qhead) * p.splits + c;
+      float* o_at = p.part + at * D + 4 * g;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        f32x4 o = O[u][dt];
+        if (FMT != KV_SAME) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_ldexpf(o[i], ve);
+        }
+        *(f32x4*)(o_at + 16 * dt) = o;
+      }
+      if (g == 0) {
+        float* ml = p.part + (long long)p.seqs.n_tokens * p.heads * p.splits * D + at * 2;
+        ml[0] = m[u];
+        ml[1] = l[u];
+      }
+    }
+  }
+}
+
+// out = the joined partials of a row, one wavefront to a row.
+template <class A, int D>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p) {
+  constexpr int E = D / 64;
+  const int lane = threadIdx.x & 63;
+  const long long i = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (i >= (long long)p.seqs.n_tokens * p.heads) return;
+  const int token = (int)(i / p.heads), qhead = (int)(i % p.heads);
+  int local;
+  const int s = paged_find(p.seqs, token, 1, 0, 0, &local);
+  if (s < 0) return;
+  const PagedSeq q = paged_load_seq(p.seqs, s, p.kv.page_shift);
+  const int t = token - q.row;
+  if (t < 0 || t >= q.done || (long long)q.n * p.group <= p.min_rows) return;
+  // the tile's positions, as the kernel above shared them out
+  const int row = t * p.group + qhead % p.group;
+  const int tile0 = row >> kManyShift << kManyShift;
+  const int rows = min(q.done * p.group - tile0, 1 << kManyShift);
+  const int kend = max(min(q.held, q.first + (tile0 + rows - 1) / p.group + 1), 0);
+  int used;
+  many_share(kend, p.splits, &used);
+  if (used == 1) return;  // written already
+  const float* part = p.part + i * p.splits * D;
+  const float* ml = p.part + (long long)p.seqs.n_tokens * p.heads * p.splits * D + i * p.splits * 2;
+  float M = -INFINITY;
+  for (int k = 0; k < used; ++k) M = fmaxf(M, ml[2 * k]);
+  float L = 0.f, o[E] = {};
+  for (int k = 0; k < used; ++k) {
+    const float mk = ml[2 * k];
+    if (mk == -INFINITY) {
+      if (M == -INFINITY) L += ml[2 * k + 1];
+      continue;
+    }
+    const float f = exp2_hw(mk - M);
+    L = fmaf(f, ml[2 * k + 1], L);
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = fmaf(f, part[k * D + E * lane + e], o[e]);
+  }
+  uint16_t* out = (uint16_t*)p.out + (long long)token * p.ldo + qhead * D + E * lane;
+#pragma unroll
+  for (int e = 0; e < E; ++e) out[e] = A::from_f32(L == 0.f ? 0.f : o[e] / L);
+}
+
 template <class A, int FMT, int D>
 hipError_t few_t(const PagedAttnParams& p, const dim3& grid, hipStream_t st) {
   hipLaunchKernelGGL((paged_few_kernel<A, FMT, D>), grid, dim3(64 * kFewWaves), 0, st, p);
@@ -510,12 +920,44 @@ hipError_t few_a(const PagedAttnParams& p, const dim3& grid, hipStream_t st) {
   return wide ? few_t<A, KV_E4M3, 128>(p, grid, st) : few_t<A, KV_E4M3, 64>(p, grid, st);
 }
 
+template <class A, int FMT, int D>
+hipError_t many_t(const PagedAttnParams& p, const dim3& grid, hipStream_t st) {
+  hipLaunchKernelGGL((paged_many_kernel<A, FMT, D>), grid, dim3(64 * kManyWaves), 0, st, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  const long long rows = (long long)p.seqs.n_tokens * p.heads;
+  hipLaunchKernelGGL((paged_join_kernel<A, D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
+template <class A>
+hipError_t many_a(const PagedAttnParams& p, const dim3& grid, hipStream_t st) {
+  const bool wide = p.kv.head_dim == 128;
+  switch (p.kv.format) {
+    case KV_SAME: return wide ? many_t<A, KV_SAME, 128>(p, grid, st) : many_t<A, KV_SAME, 64>(p, grid, st);
+    case KV_I8: return wide ? many_t<A, KV_I8, 128>(p, grid, st) : many_t<A, KV_I8, 64>(p, grid, st);
+  }
+  return wide ? many_t<A, KV_E4M3, 128>(p, grid, st) : many_t<A, KV_E4M3, 64>(p, grid, st);
+}
+
+// A sequence's rows per key/value head (new tokens x heads of the group) up to which it goes to
+// the kernel for few rows when a batch needs both.
+constexpr int kFewRows = 32;
+
 // Splits of a sequence that the partials have room for: kMaxPartials rows of all chunks.
 constexpr long long kMaxPartials = 1 << 18;
 int few_splits(const PagedCache& kv, const PagedSeqs& b, int heads) {
   const long long rows = (long long)b.n_tokens * heads;
   if (rows * 2 > kMaxPartials || paged_tiles(b, heads / kv.heads, kFewShift, 1) * kv.heads > kPagedCounters) return 1;
   return (int)std::min<long long>(kPagedMaxSplits, kMaxPartials / rows);
+}
+
+// Workgroups that share a tile of the kernel for many rows.
+int many_splits(const PagedCache& kv, const PagedSeqs& b, int heads) {
+  const long long tiles = paged_tiles(b, heads / kv.heads, kManyShift, 1) * kv.heads;
+  const long long cap = (long long)b.max_pages << kv.page_shift;
+  const long long most = std::min<long long>(kManyMaxSplits, (cap + 4 * kManyKeys - 1) / (4 * kManyKeys));
+  return (int)std::max<long long>(1, std::min(most, kManyWorkgroups / tiles));
 }
 
 }  // namespace
@@ -525,22 +967,39 @@ size_t paged_ws_bytes(const PagedCache& kv, const PagedSeqs& b, int heads) {
   const long long chunks = std::min<long long>((cap + 127) / 128, kPagedMaxSplits);
   const long long rows = (long long)b.n_tokens * heads;
   const long long few = std::min(rows * chunks, kMaxPartials);
-  return kPagedCounters * sizeof(uint32_t) + (size_t)few * (kv.head_dim + 2) * sizeof(float);
+  // a split tile is one of at most kManyWorkgroups, of 128 rows
+  const long long many = std::min<long long>(rows * kManyMaxSplits, (long long)kManyWorkgroups << kManyShift);
+  return kPagedCounters * sizeof(uint32_t) + (size_t)std::max(few, many) * (kv.head_dim + 2) * sizeof(float);
 }
 
 hipError_t launch_paged_attention(PagedAttnParams p, double scale, void* ws, hipStream_t stream) {
-  if (p.seqs.n_tokens < 1 || p.seqs.n_seq < 1) return hipSuccess;
+  const PagedSeqs& b = p.seqs;
+  if (b.n_tokens < 1 || b.n_seq < 1) return hipSuccess;
   p.group = p.heads / p.kv.heads;
   p.scale = (float)(scale * (double)kLog2e);
   p.cnt = (uint32_t*)ws;
   p.part = (float*)(p.cnt + kPagedCounters);
-  const long long cap = (long long)p.seqs.max_pages << p.kv.page_shift;
-  p.splits = few_splits(p.kv, p.seqs, p.heads);
-  p.splits = (int)std::min<long long>(p.splits, (cap + 127) / 128);
-  p.min_rows = 0;
-  p.max_rows = 0x7FFFFFFF;
-  const dim3 grid((unsigned)(paged_tiles(p.seqs, p.group, kFewShift, 1) * p.kv.heads), (unsigned)p.splits);
-  return p.kv.dtype == 1 ? few_a<BF16>(p, grid, stream) : few_a<F16>(p, grid, stream);
+  // Rows of the longest sequence, and, if every row belongs to one, of the shortest: a batch of
+  // short ones only or of long ones only takes one kernel.
+  const long long longest = (long long)std::min(b.max_new, b.n_tokens) * p.group;
+  const long long shortest = (b.n_tokens - (b.n_seq - 1LL) * b.max_new) * p.group;
+  const bool many = longest > kFewRows, few = !many || shortest <= kFewRows;
+  hipError_t e = hipSuccess;
+  if (few) {
+    const long long cap = (long long)b.max_pages << p.kv.page_shift;
+    p.splits = (int)std::min<long long>(few_splits(p.kv, b, p.heads), (cap + 127) / 128);
+    p.min_rows = 0;
+    p.max_rows = many ? kFewRows : 0x7FFFFFFF;
+    const dim3 grid((unsigned)(paged_tiles(b, p.group, kFewShift, 1) * p.kv.heads), (unsigned)p.splits);
+    e = p.kv.dtype == 1 ? few_a<BF16>(p, grid, stream) : few_a<F16>(p, grid, stream);
+  }
+  if (e == hipSuccess && many) {
+    p.splits = many_splits(p.kv, b, p.heads);
+    p.min_rows = few ? kFewRows : 0;
+    const dim3 grid((unsigned)(paged_tiles(b, p.group, kManyShift, 1) * p.kv.heads), (unsigned)p.splits);
+    e = p.kv.dtype == 1 ? many_a<BF16>(p, grid, stream) : many_a<F16>(p, grid, stream);
+  }
+  return e;
 }
 
 }  // namespace hg
