@@ -96,13 +96,22 @@ __host__ __device__ inline PagedTile paged_tile(const PagedSeq& q, int local) {
 }
 
 // Positions per workgroup of the kernel for few rows, at a sequence whose cache holds `held`
-// positions and at most `splits` workgroups to a sequence.
+// positions: a share of `even` of them (as many as fill the device), but at least 128 and at most
+// kPagedMaxChunk (a long sequence among short ones is cut finer), unless that makes more than `most`.
 constexpr int kPagedMaxSplits = 64;
-__host__ __device__ inline int paged_chunk(int held, int splits) {
-  const int unit = held <= 1024 ? 128 : held <= 8192 ? 256 : 512;
-  const int most = splits < kPagedMaxSplits ? splits : kPagedMaxSplits;
-  const int even = (held / most + 128) & ~127;  // at least held / most
-  return even > unit ? even : unit;
+constexpr int kPagedMaxChunk = 2048;
+__host__ __device__ inline int paged_chunk(int held, int even, int most) {
+  const int share = (held / even + 128) & ~127;  // more than held / even
+  const int least = (held / most + 128) & ~127;
+  const int chunk = share < kPagedMaxChunk ? share : kPagedMaxChunk;
+  return chunk > least ? chunk : least;
+}
+// The most workgroups that share a sequence of up to `cap` positions.
+inline int paged_chunks(long long cap, int even, int most) {
+  long long n = cap / kPagedMaxChunk + 1;
+  if (n < even) n = even;
+  if (n > (cap + 127) / 128) n = (cap + 127) / 128;
+  return (int)(n < most ? n : most);
 }
 
 // ---- launches ----
@@ -131,7 +140,8 @@ struct PagedAttnParams {
   float scale;    // set by the launcher: the caller's scale times log2 e
   uint32_t* cnt;  // kPagedCounters arrival counters, zero between launches
   float* part;    // partial results of split sequences
-  int splits;     // set by the launcher
+  int splits;     // set by the launcher: the most workgroups that share a sequence's positions
+  int even, most; // set by the launcher: see paged_chunk
   int min_rows;   // set by the launcher: sequences with more than min_rows rows per key/value head
   int max_rows;   // and at most max_rows are worked on
 };

@@ -25,6 +25,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace hg {
 namespace {
@@ -163,54 +164,60 @@ __device__ __forceinline__ float load_through(const float* p) {
 
 // ---- few rows: one token of a sequence, or some ----
 //
-// Workgroup (tile of 16 rows, key/value head, chunk of positions) of four wavefronts, each with
+// Workgroup (tile of 16 U rows, key/value head, chunk of positions) of four wavefronts, each with
 // 32 positions at a time; keys and values go from memory straight into the products' operands,
-// 1 KiB a load.  The wavefronts' sums meet in LDS; a sequence of several chunks leaves partials
-// [m, l, o] in the workspace and the last workgroup of (tile, head) to arrive joins them in chunk
-// order (an arrival counter, no waiting), so results do not depend on timing.
+// 1 KiB a load, and feed U products.  The wavefronts' sums meet in LDS; a sequence of several
+// chunks leaves partials [m, l, o] in the workspace and the last workgroup of (tile, head) to arrive
+// joins them in chunk order (an arrival counter, no waiting), so results do not depend on timing.
 constexpr int kFewWaves = 4;
-constexpr int kFewShift = 4;  // rows per tile: 16
+template <int U>
+constexpr int kFewShift = U == 2 ? 5 : 4;  // rows per tile: 16 U
 
-template <class A, int FMT, int D>
-__global__ __launch_bounds__(64 * kFewWaves, 2) void paged_few_kernel(PagedAttnParams p) {
+template <class A, int FMT, int D, int U>
+__global__ __launch_bounds__(64 * kFewWaves, U == 2 ? 2 : D == 128 ? 3 : 4) void paged_few_kernel(PagedAttnParams p) {
   typedef typename Compute<A, FMT>::type T;
   constexpr int ES = FMT == KV_SAME ? 2 : 1;
-  constexpr int KK = D / 32, DT = D / 16;
+  constexpr int KK = D / 32, DT = D / 16, R = 16 * U;
   constexpr int NL = 32 * D * ES / 1024;   // loads of 32 positions' keys (or values)
   constexpr int OS = D + 4;
-  __shared__ __align__(16) float sacc[kFewWaves][16][OS];
-  __shared__ float sm[kFewWaves][16], sl[kFewWaves][16];
+  __shared__ __align__(16) float sacc[kFewWaves][R][OS];
+  __shared__ float sm[kFewWaves][R], sl[kFewWaves][R];
   __shared__ int s_last;
 
   const int head = blockIdx.x % p.kv.heads, tile = blockIdx.x / p.kv.heads;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g = lane >> 4;
   int local;
-  const int s = __builtin_amdgcn_readfirstlane(paged_find(p.seqs, tile, p.group, kFewShift, 1, &local));
+  PagedSeq q;
+  const int s = paged_find(p.seqs, p.kv.page_shift, tile, p.group, kFewShift<U>, 1, &local, &q);
   if (s < 0) return;
-  const PagedSeq q = paged_load_seq(p.seqs, s, p.kv.page_shift);
   if ((long long)q.n * p.group <= p.min_rows || (long long)q.n * p.group > p.max_rows) return;
-  const int row0 = local << kFewShift;
-  const int rows = min(q.done * p.group - row0, 16);  // of this tile
+  const int row0 = local << kFewShift<U>;
+  const int rows = min(q.done * p.group - row0, R);  // of this tile
   if (rows <= 0) return;
   // a token at position t sees positions [0, t]; the tile's last one sees the most
   const int last = q.first + (row0 + rows - 1) / p.group;
   const int kend = max(min(q.held, last + 1), 0);
-  const int chunk = paged_chunk(q.held, p.splits);
+  const int chunk = paged_chunk(q.held, p.even, p.most);
   const int nchunk = max((kend + chunk - 1) / chunk, 1);
   const int c = blockIdx.y;
   if (c >= nchunk) return;
   const int j0 = c * chunk, j1 = min(j0 + chunk, kend);
   const int nsteps = (max(j1 - j0, 0) + 31) >> 5;
 
-  const int row = row0 + col;
-  const int mypos = col < rows ? q.first + row / p.group : -1;
   const int minpos = q.first + row0 / p.group;  // the least a row of the tile sees to
-  const int qhead = head * p.group + row % p.group;
-  u32x4 qf[KK];
-  float mult;
-  load_query<A, FMT, D>((const uint16_t*)p.q + (long long)(q.row + row / p.group) * p.ldq + qhead * D + 8 * g,
-                        col < rows, p.scale, qf, &mult);
+  int mypos[U];
+  u32x4 qf[U][KK];
+  float mult[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int row = row0 + 16 * u + col;
+    const bool ok = 16 * u + col < rows;
+    mypos[u] = ok ? q.first + row / p.group : -1;
+    load_query<A, FMT, D>((const uint16_t*)p.q + (long long)(q.row + row / p.group) * p.ldq +
+                              (head * p.group + row % p.group) * D + 8 * g,
+                          ok, p.scale, qf[u], &mult[u]);
+  }
 
   const long long P = p.kv.page_size;
   const int pmask = p.kv.page_size - 1;
@@ -219,10 +226,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_few_kernel(PagedAttnP
 
   u32x4 kr[NL], vr[NL];
   f32x4 ksc[2], vsc[2];
-  float m, l;
-  uint32_t seen;
+  float m[U], l[U];
+  uint32_t seen[U];
   int ve;  // values' scales are taken relative to 2^ve
-  f32x4 O[DT];
+  f32x4 O[U][DT];
 
   // lane i holds the page of this wavefront's step number n0 + i
   int pages = -1;
@@ -253,19 +260,25 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_few_kernel(PagedAttnP
     }
   };
 
-  for (bool careful = false;; careful = true) {
-    m = -INFINITY;
-    l = 0.f;
-    seen = 0;
+  auto walk = [&](auto again) {
+    constexpr bool careful = decltype(again)::value;
     ve = -126;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) O[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < U; ++u) {
+      m[u] = -INFINITY;
+      l[u] = 0.f;
+      seen[u] = 0;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) O[u][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     int page = -1, n = 0;
     if (wave < nsteps) {
       look_up(0);
       page = __builtin_amdgcn_readlane(pages, 0);
-      load_keys(page, j0 + 32 * wave);
-      load_values(page, j0 + 32 * wave);
+      if (!careful) {
+        load_keys(page, j0 + 32 * wave);
+        load_values(page, j0 + 32 * wave);
+      }
     }
     for (int st = wave; st < nsteps; st += kFewWaves) {
       const int jb = j0 + 32 * st;
@@ -275,11 +288,13 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_few_kernel(PagedAttnP
         if ((++n & 63) == 0) look_up(n);
         next = __builtin_amdgcn_readlane(pages, n & 63);
       }
+      if (careful) load_keys(page, jb);  // nothing ahead of its use: fewer registers
       // scores
-      f32x4 sc[2];
+      f32x4 sc[U][2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < U; ++u) sc[u][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < KK; ++k) {
           u32x4 kf;
@@ -289,127 +304,147 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_few_kernel(PagedAttnP
             const u32x4& w = kr[t * (KK / 2) + (k >> 1)];
             kf = codes_f16<FMT>(w[2 * (k & 1)], w[2 * (k & 1) + 1]);
           }
-          acc = T::mfma(kf, qf[k], acc);
+#pragma unroll
+          for (int u = 0; u < U; ++u) sc[u][t] = T::mfma(kf, qf[u][k], sc[u][t]);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sc[t][i] = FMT == KV_SAME ? acc[i] * mult : acc[i] * (mult * ksc[t][i]);
+        for (int u = 0; u < U; ++u) {
+          if (FMT == KV_SAME) sc[u][t] *= mult[u];
+          else sc[u][t] *= mult[u] * ksc[t];
+        }
       }
-      if (more) load_keys(next, jb + 32 * kFewWaves);
+      if (more && !careful) load_keys(next, jb + 32 * kFewWaves);
+      if (careful) load_values(page, jb);
       // the last positions, and positions of a page that is not there, are masked
       const bool whole = page >= 0 && jb + 32 <= q.held;
       const bool full = whole && jb + 31 <= minpos;
       const int top = (page >= 0 ? q.held - 1 : -1) - (jb + 4 * g);  // element e is held if up to here
-      uint32_t vis = 0xFFu;
-      if (!full) {
-        const int to = min(mypos - (jb + 4 * g), top);
-        vis = 0u;
+      uint32_t vis[U];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const bool see = 16 * (e >> 2) + (e & 3) <= to;
-          vis |= (see ? 1u : 0u) << e;
-          sc[e >> 2][e & 3] = see ? sc[e >> 2][e & 3] : -INFINITY;
+      for (int u = 0; u < U; ++u) {
+        vis[u] = 0xFFu;
+        if (!full) {
+          const int to = min(mypos[u] - (jb + 4 * g), top);
+          vis[u] = 0u;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const bool see = 16 * (e >> 2) + (e & 3) <= to;
+            vis[u] |= (see ? 1u : 0u) << e;
+            sc[u][e >> 2][e & 3] = see ? sc[u][e >> 2][e & 3] : -INFINITY;
+          }
         }
+        seen[u] |= vis[u];
       }
-      seen |= vis;
-      float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
-                       fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
-      mx = fmaxf(m, groups_max(mx));
-      const float ms = mx == -INFINITY ? 0.f : mx;
-      float al = exp2_hw(m - ms);
-      m = mx;
-      float w[8], sum = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        w[e] = exp2_hw(sc[e >> 2][e & 3] - ms);
-        sum += w[e];
-      }
-      l = fmaf(l, al, sum);
+      f32x4 vs[2];
+      int e2 = ve;
       if (FMT != KV_SAME) {
         uint32_t most = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           most = max(most, 16 * (e >> 2) + (e & 3) <= top ? finite_bits(vsc[e >> 2][e & 3]) : 0u);
-        const int e2 = max(ve, (int)(groups_umax(most) >> 23) - 126);
-        al = __builtin_amdgcn_ldexpf(al, ve - e2);
-        ve = e2;
+        e2 = max(ve, (int)(groups_umax(most) >> 23) - 126);
+        const float to = __builtin_amdgcn_ldexpf(1.f, -e2);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float r = w[e] * __builtin_amdgcn_ldexpf(vsc[e >> 2][e & 3], -ve);
-          w[e] = (vis >> e) & 1 ? r : 0.f;
-        }
-      }
-      if (__ballot(al != 1.f)) {
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) O[dt][i] *= al;
-      }
-      // weights to 16 bits twice: a second product takes what the first rounding left (memory is
-      // what bounds this kernel), so that weights count as in binary32 but for fp16's smallest step
-      u32x4 pf, pl;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        pf[i] = T::pack(w[2 * i], w[2 * i + 1]);
-        pl[i] = T::pack(w[2 * i] - T::to_f32(pf[i] & 0xFFFFu), w[2 * i + 1] - T::to_f32(pf[i] >> 16));
-      }
-      u32x4 vf[DT];
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        if (FMT == KV_SAME) vf[dt] = vr[dt];
-        else vf[dt] = codes_f16<FMT>(vr[dt >> 1][2 * (dt & 1)], vr[dt >> 1][2 * (dt & 1) + 1]);
+        for (int t = 0; t < 2; ++t) vs[t] = vsc[t] * to;
       }
       if (!whole) {
         // what lies behind a sequence's end was never written: it may be anything
         u32x4 keep;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int to = top - (16 * (i >> 1) + 2 * (i & 1));
-          keep[i] = (to >= 0 ? 0xFFFFu : 0u) | (to >= 1 ? 0xFFFF0000u : 0u);
+          if (FMT == KV_SAME) {  // elements 2 i and 2 i + 1 of a dimension
+            const int to = top - (16 * (i >> 1) + 2 * (i & 1));
+            keep[i] = (to >= 0 ? 0xFFFFu : 0u) | (to >= 1 ? 0xFFFF0000u : 0u);
+          } else {  // elements 4 (i % 2) + [0, 4) of one of two dimensions
+            const int to = top - 16 * (i & 1);
+            keep[i] = to >= 3 ? ~0u : to < 0 ? 0u : ~0u >> (24 - 8 * to);
+          }
         }
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) vf[dt] &= keep;
+        for (int i = 0; i < NL; ++i) vr[i] &= keep;
       }
-      if (FMT == KV_SAME && careful) {
-        const u32x4 sees = seen_keys<T>(vis);
+      auto fragment = [&](int dt) {
+        if (FMT == KV_SAME) return vr[dt];
+        return codes_f16<FMT>(vr[dt >> 1][2 * (dt & 1)], vr[dt >> 1][2 * (dt & 1) + 1]);
+      };
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float mx = fmaxf(fmaxf(fmaxf(sc[u][0][0], sc[u][0][1]), fmaxf(sc[u][0][2], sc[u][0][3])),
+                         fmaxf(fmaxf(sc[u][1][0], sc[u][1][1]), fmaxf(sc[u][1][2], sc[u][1][3])));
+        mx = fmaxf(m[u], groups_max(mx));
+        const float ms = mx == -INFINITY ? 0.f : mx;
+        float al = exp2_hw(m[u] - ms), w[8], sum = 0.f;
+        m[u] = mx;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          w[e] = exp2_hw(sc[u][e >> 2][e & 3] - ms);
+          sum += w[e];
+        }
+        l[u] = fmaf(l[u], al, sum);
+        if (FMT != KV_SAME) {
+          al = __builtin_amdgcn_ldexpf(al, ve - e2);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[e] = vis[u] >> e & 1u ? w[e] * vs[e >> 2][e & 3] : 0.f;
+        }
+        if (__ballot(al != 1.f)) {
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) O[u][dt] *= al;
+        }
+        // weights to 16 bits twice: a second product takes what the first rounding left (memory is
+        // what bounds this kernel), so that weights count as in binary32 but for fp16's smallest step
+        u32x4 pf, pl;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          pf[i] = T::pack(w[2 * i], w[2 * i + 1]);
+          pl[i] = T::pack(w[2 * i] - T::to_f32(pf[i] & 0xFFFFu), w[2 * i + 1] - T::to_f32(pf[i] >> 16));
+        }
+        const u32x4 sees = seen_keys<T>(vis[u]);
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
-          f32x4* const o[1] = {&O[dt]};
-          take_nonfinite<T, 1>(vf[dt], &sees, o);
+          u32x4 vf = fragment(dt);
+          if (careful) {
+            f32x4* const o[1] = {&O[u][dt]};
+            take_nonfinite<T, 1>(vf, &sees, o);
+          }
+          O[u][dt] = T::mfma(vf, pl, T::mfma(vf, pf, O[u][dt]));
         }
       }
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        O[dt] = T::mfma(vf[dt], pf, O[dt]);
-        O[dt] = T::mfma(vf[dt], pl, O[dt]);
-      }
-      if (more) load_values(next, jb + 32 * kFewWaves);
+      ve = e2;
+      if (more && !careful) load_values(next, jb + 32 * kFewWaves);
       page = next;
     }
-    if (FMT != KV_SAME || careful) break;
+  };
+  walk(std::false_type{});
+  if (FMT == KV_SAME) {
     bool odd = false;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) odd |= !(fabsf(O[dt][i]) < INFINITY);
-    if (!__ballot(odd)) break;
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) odd |= !(fabsf(O[u][dt][i]) < INFINITY);
+    if (__ballot(odd)) walk(std::true_type{});
   }
 
-  // a row that saw positions, all of score -infinity, has no softmax: NaN, as the formula has it
-  l = groups_sum(l);
-  if (m == -INFINITY && groups_umax(seen) != 0) l = NAN;
-  if (col < rows) {
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    // a row that saw positions, all of score -infinity, has no softmax: NaN, as the formula has it
+    l[u] = groups_sum(l[u]);
+    if (m[u] == -INFINITY && groups_umax(seen[u]) != 0) l[u] = NAN;
+    const int r = 16 * u + col;
+    if (r >= rows) continue;
     if (g == 0) {
-      sm[wave][col] = m;
-      sl[wave][col] = l;
+      sm[wave][r] = m[u];
+      sl[wave][r] = l[u];
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      f32x4 o = O[dt];
+      f32x4 o = O[u][dt];
       if (FMT != KV_SAME) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_ldexpf(o[i], ve);
       }
-      *(f32x4*)&sacc[wave][col][16 * dt + 4 * g] = o;
+      *(f32x4*)&sacc[wave][r][16 * dt + 4 * g] = o;
     }
   }
   __syncthreads();
@@ -472,8 +507,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_few_kernel(PagedAttnP
   __syncthreads();
   if (!s_last) return;
   // join the chunks, in order; weights of a row's chunks in LDS
-  float* weight = &sacc[0][0][0];  // [16][kPagedMaxSplits]
-  static_assert(16 * kPagedMaxSplits <= kFewWaves * 16 * OS, "chunk weights");
+  float* weight = &sacc[0][0][0];  // [R][kPagedMaxSplits]
+  static_assert(kPagedMaxSplits <= kFewWaves * OS, "chunk weights");
   for (int i = threadIdx.x; i < rows * nchunk; i += 64 * kFewWaves) {
     const int r = i / nchunk, k = i % nchunk;
     weight[r * kPagedMaxSplits + k] = load_through(part_at(r) + (long long)k * (D + 2));
@@ -547,9 +582,9 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g = lane >> 4;
   int local;
-  const int s = __builtin_amdgcn_readfirstlane(paged_find(p.seqs, tile, p.group, kManyShift, 1, &local));
+  PagedSeq q;
+  const int s = paged_find(p.seqs, p.kv.page_shift, tile, p.group, kManyShift, 1, &local, &q);
   if (s < 0) return;
-  const PagedSeq q = paged_load_seq(p.seqs, s, p.kv.page_shift);
   if ((long long)q.n * p.group <= p.min_rows) return;
   const int all = q.done * p.group;
   local = ((all + (1 << kManyShift) - 1) >> kManyShift) - 1 - local;  // the rows that see most come first
@@ -633,7 +668,8 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
       if (lane < 32) scales[b][side * kManyKeys + 32 * half + lane] = raw_scale;
     }
   };
-  auto compute = [&](const char* buf, int b, int step, int pa, int pb, bool careful) {
+  auto compute = [&](const char* buf, int b, int step, int pa, int pb, auto again) {
+    constexpr bool careful = decltype(again)::value;
     const int jb = j0 + kManyKeys * step;
     if (jb > wmax) return;
     const char* kb = buf + lane * 16;
@@ -733,32 +769,15 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
         for (int i = 0; i < 4; ++i) pf[u][h][i] = T::pack(w[8 * h + 2 * i], w[8 * h + 2 * i + 1]);
     }
     ve = e2;
-    if (whole && !careful) {
-#pragma unroll
-      for (int h = 0; h < KT / 2; ++h)
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const u32x4 vf = *(const u32x4*)(vb + h * (kSide / 2) + dt * 1024);
-#pragma unroll
-          for (int u = 0; u < U; ++u) O[u][dt] = T::mfma(vf, pf[u][h], O[u][dt]);
-        }
-      return;
-    }
-    // what lies behind a sequence's end was never written: it may be anything
 #pragma unroll
     for (int h = 0; h < KT / 2; ++h) {
-      u32x4 keep, sees[U];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int to = top[h] - (jl + 32 * h + 16 * (i >> 1) + 2 * (i & 1));
-        keep[i] = (to >= 0 ? 0xFFFFu : 0u) | (to >= 1 ? 0xFFFF0000u : 0u);
-      }
+      u32x4 sees[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) sees[u] = seen_keys<T>(vis[u] >> (8 * h));
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
-        u32x4 vf = *(const u32x4*)(vb + h * (kSide / 2) + dt * 1024) & keep;
-        if (FMT == KV_SAME && careful) {
+        u32x4 vf = *(const u32x4*)(vb + h * (kSide / 2) + dt * 1024);
+        if (careful) {
           f32x4* const o[2] = {&O[0][dt], &O[1][dt]};
           take_nonfinite<T, U>(vf, sees, o);
         }
@@ -767,8 +786,23 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
       }
     }
   };
+  // what lies behind a sequence's end was never written and may be anything: zeros for its values
+  auto blank = [&](char* buf, int step, int pa, int pb) {
+    for (int i = threadIdx.x; i < kSide / 16; i += 64 * kManyWaves) {
+      const int half = i >= kSide / 32, vg = (i & 63) >> 4;
+      const int top = ((half ? pb : pa) >= 0 ? q.held - 1 : -1) - (j0 + kManyKeys * step + 32 * half + 4 * vg);
+      u32x4* at = (u32x4*)(buf + kSide) + i;
+      u32x4 v = *at;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int to = top - (16 * (w >> 1) + 2 * (w & 1));
+        v[w] &= (to >= 0 ? 0xFFFFu : 0u) | (to >= 1 ? 0xFFFF0000u : 0u);
+      }
+      *at = v;
+    }
+  };
 
-  for (bool careful = false;; careful = true) {
+  auto walk = [&](auto again) {
     ve = -126;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -794,7 +828,11 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
         half_pages(step + 1, &na, &nb);
         issue(other, step + 1, na, nb);
       }
-      compute(now, b, step, pa, pb, careful);
+      if (pa < 0 || pb < 0 || j0 + kManyKeys * (step + 1) > q.held) {
+        blank(now, step, pa, pb);
+        __syncthreads();
+      }
+      compute(now, b, step, pa, pb, again);
       if (more) commit(other, 1 - b);
       pa = na;
       pb = nb;
@@ -803,7 +841,9 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
       turn(buf0, buf1, 0, step);
       if (step + 1 < nsteps) turn(buf1, buf0, 1, step + 1);
     }
-    if (FMT != KV_SAME || careful) break;
+  };
+  walk(std::false_type{});
+  if (FMT == KV_SAME) {
     bool odd = false;
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -816,7 +856,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
     __syncthreads();
     if (__ballot(odd) && lane == 0) s_odd = 1;
     __syncthreads();
-    if (!s_odd) break;
+    if (s_odd) walk(std::true_type{});
   }
 
 #pragma unroll
@@ -870,9 +910,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p) {
   if (i >= (long long)p.seqs.n_tokens * p.heads) return;
   const int token = (int)(i / p.heads), qhead = (int)(i % p.heads);
   int local;
-  const int s = paged_find(p.seqs, token, 1, 0, 0, &local);
-  if (s < 0) return;
-  const PagedSeq q = paged_load_seq(p.seqs, s, p.kv.page_shift);
+  PagedSeq q;
+  if (paged_find(p.seqs, p.kv.page_shift, token, 1, 0, 0, &local, &q) < 0) return;
   const int t = token - q.row;
   if (t < 0 || t >= q.done || (long long)q.n * p.group <= p.min_rows) return;
   // the tile's positions, as the kernel above shared them out
@@ -905,19 +944,21 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p) {
 }
 
 template <class A, int FMT, int D>
-hipError_t few_t(const PagedAttnParams& p, const dim3& grid, hipStream_t st) {
-  hipLaunchKernelGGL((paged_few_kernel<A, FMT, D>), grid, dim3(64 * kFewWaves), 0, st, p);
+hipError_t few_t(PagedAttnParams p, bool wide, unsigned tiles, hipStream_t st) {
+  const dim3 grid(tiles, p.splits);
+  if (wide) hipLaunchKernelGGL((paged_few_kernel<A, FMT, D, 2>), grid, dim3(64 * kFewWaves), 0, st, p);
+  else hipLaunchKernelGGL((paged_few_kernel<A, FMT, D, 1>), grid, dim3(64 * kFewWaves), 0, st, p);
   return hipGetLastError();
 }
 
 template <class A>
-hipError_t few_a(const PagedAttnParams& p, const dim3& grid, hipStream_t st) {
-  const bool wide = p.kv.head_dim == 128;
+hipError_t few_a(const PagedAttnParams& p, bool wide, unsigned tiles, hipStream_t st) {
+  const bool d128 = p.kv.head_dim == 128;
   switch (p.kv.format) {
-    case KV_SAME: return wide ? few_t<A, KV_SAME, 128>(p, grid, st) : few_t<A, KV_SAME, 64>(p, grid, st);
-    case KV_I8: return wide ? few_t<A, KV_I8, 128>(p, grid, st) : few_t<A, KV_I8, 64>(p, grid, st);
+    case KV_SAME: return d128 ? few_t<A, KV_SAME, 128>(p, wide, tiles, st) : few_t<A, KV_SAME, 64>(p, wide, tiles, st);
+    case KV_I8: return d128 ? few_t<A, KV_I8, 128>(p, wide, tiles, st) : few_t<A, KV_I8, 64>(p, wide, tiles, st);
   }
-  return wide ? few_t<A, KV_E4M3, 128>(p, grid, st) : few_t<A, KV_E4M3, 64>(p, grid, st);
+  return d128 ? few_t<A, KV_E4M3, 128>(p, wide, tiles, st) : few_t<A, KV_E4M3, 64>(p, wide, tiles, st);
 }
 
 template <class A, int FMT, int D>
@@ -944,12 +985,18 @@ hipError_t many_a(const PagedAttnParams& p, const dim3& grid, hipStream_t st) {
 // the kernel for few rows when a batch needs both.
 constexpr int kFewRows = 32;
 
-// Splits of a sequence that the partials have room for: kMaxPartials rows of all chunks.
+// How the kernel for few rows deals a batch: kFewWorkgroups of even chunks fill the device (3 to 4
+// workgroups on each of 256 CUs), as far as the partials (kMaxPartials rows of all chunks) and the
+// counters go.
+constexpr int kFewWorkgroups = 1024;
 constexpr long long kMaxPartials = 1 << 18;
-int few_splits(const PagedCache& kv, const PagedSeqs& b, int heads) {
-  const long long rows = (long long)b.n_tokens * heads;
-  if (rows * 2 > kMaxPartials || paged_tiles(b, heads / kv.heads, kFewShift, 1) * kv.heads > kPagedCounters) return 1;
-  return (int)std::min<long long>(kPagedMaxSplits, kMaxPartials / rows);
+void few_splits(PagedAttnParams* p, long long tiles) {
+  const long long cap = (long long)p->seqs.max_pages << p->kv.page_shift;
+  const long long rows = (long long)p->seqs.n_tokens * p->heads;
+  const long long room = tiles > kPagedCounters ? 1 : std::max<long long>(1, kMaxPartials / rows);
+  p->most = (int)std::min<long long>(room, kPagedMaxSplits);
+  p->even = (int)std::min<long long>(std::max<long long>(1, (kFewWorkgroups + tiles / 2) / tiles), p->most);
+  p->splits = paged_chunks(cap, p->even, p->most);
 }
 
 // Workgroups that share a tile of the kernel for many rows.
@@ -986,12 +1033,12 @@ hipError_t launch_paged_attention(PagedAttnParams p, double scale, void* ws, hip
   const bool many = longest > kFewRows, few = !many || shortest <= kFewRows;
   hipError_t e = hipSuccess;
   if (few) {
-    const long long cap = (long long)b.max_pages << p.kv.page_shift;
-    p.splits = (int)std::min<long long>(few_splits(p.kv, b, p.heads), (cap + 127) / 128);
+    const bool wide = longest > 16;
+    const long long tiles = paged_tiles(b, p.group, wide ? kFewShift<2> : kFewShift<1>, 1) * p.kv.heads;
+    few_splits(&p, tiles);
     p.min_rows = 0;
     p.max_rows = many ? kFewRows : 0x7FFFFFFF;
-    const dim3 grid((unsigned)(paged_tiles(b, p.group, kFewShift, 1) * p.kv.heads), (unsigned)p.splits);
-    e = p.kv.dtype == 1 ? few_a<BF16>(p, grid, stream) : few_a<F16>(p, grid, stream);
+    e = p.kv.dtype == 1 ? few_a<BF16>(p, wide, (unsigned)tiles, stream) : few_a<F16>(p, wide, (unsigned)tiles, stream);
   }
   if (e == hipSuccess && many) {
     p.splits = many_splits(p.kv, b, p.heads);

@@ -86,25 +86,30 @@ __device__ __forceinline__ float groups_sum(float v) {
 }
 
 // Sequence of a tile (see paged_tile_base), the same in every lane of the wavefront: the last
-// one whose tiles begin at or before it, or -1; *local the tile's number within it.
-__device__ __forceinline__ int paged_find(const PagedSeqs& b, int tile, int unit, int shift, int extra, int* local) {
+// one whose tiles begin at or before it, or -1; *local the tile's number within it, *seq its
+// rows and positions.  64 sequences at a time, in one round of loads.
+__device__ __forceinline__ int paged_find(const PagedSeqs& b, int page_shift, int tile, int unit, int shift, int extra,
+                                          int* local, PagedSeq* seq) {
   const int lane = threadIdx.x & 63;
-  int count = 0;
+  int s = -1, start = 0, end = 0, len = 0;
   for (int i0 = 0; i0 < b.n_seq; i0 += 64) {
-    const int i = i0 + lane;
-    const bool before =
-        i < b.n_seq && paged_tile_base(load_i32(b.start + i), i, b.n_tokens, unit, shift, extra) <= tile;
+    const int i = min(i0 + lane, b.n_seq - 1);
+    const int st = load_i32(b.start + i), en = load_i32(b.start + i + 1), ln = load_i32(b.len + i);
+    const bool before = i0 + lane < b.n_seq && paged_tile_base(st, i, b.n_tokens, unit, shift, extra) <= tile;
     const int c = __popcll(__ballot(before));
-    count += c;
+    if (c > 0) {
+      s = i0 + c - 1;
+      start = __builtin_amdgcn_readlane(st, c - 1);
+      end = __builtin_amdgcn_readlane(en, c - 1);
+      len = __builtin_amdgcn_readlane(ln, c - 1);
+    }
     if (c < 64) break;
   }
-  const int s = count - 1;
-  *local = s < 0 ? 0 : tile - paged_tile_base(load_i32(b.start + s), s, b.n_tokens, unit, shift, extra);
-  return *local < 0 ? -1 : s;  // (negative only where new_start decreases)
-}
-
-__device__ __forceinline__ PagedSeq paged_load_seq(const PagedSeqs& b, int s, int page_shift) {
-  return paged_seq(load_i32(b.start + s), load_i32(b.start + s + 1), load_i32(b.len + s), b, page_shift);
+  if (s < 0) return -1;
+  *local = tile - paged_tile_base(start, s, b.n_tokens, unit, shift, extra);
+  if (*local < 0) return -1;  // (only where new_start decreases)
+  *seq = paged_seq(start, end, len, b, page_shift);
+  return s;
 }
 
 // Page of position j (j < held) of sequence s; -1 where the table names none.

@@ -102,9 +102,9 @@ struct Tile {
 
 __device__ __forceinline__ bool find_tile(const PagedCopyParams& p, int head, Tile* t) {
   int local;
-  const int s = paged_find(p.seqs, blockIdx.x, 1, 5, 2, &local);
+  PagedSeq q;
+  const int s = paged_find(p.seqs, p.kv.page_shift, blockIdx.x, 1, 5, 2, &local, &q);
   if (s < 0) return false;
-  const PagedSeq q = paged_load_seq(p.seqs, s, p.kv.page_shift);
   const PagedTile u = paged_tile(q, local);
   if (u.hi <= u.lo) return false;
   t->row = u.row;

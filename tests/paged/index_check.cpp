@@ -115,12 +115,14 @@ int main() {
           CHECK(hits[start[s] + i] == (i < b.max_new && len[s] - n + i >= 0 ? 1 : 0));
         }
 
-    // chunks of a sequence: no more than its splits, whole steps, nothing left over
-    const int held = pick(0, 1) ? pick(0, 3000) : pick(0, 1 << 30), splits = pick(1, 64);
-    const int most = std::min<long long>(splits, ((long long)held + 127) / 128);
-    const int chunk = paged_chunk(held, splits);
+    // chunks of a sequence: no more than its cap allows, whole steps, nothing left over
+    const int cap = pick(0, 1) ? pick(1, 100) * 32 : pick(1, 1 << 25) * 32;
+    const int most = pick(1, kPagedMaxSplits), even = pick(1, most);
+    const int held = std::min(cap, pick(0, 1) ? pick(0, 3000) : pick(0, 1 << 30));
+    const int chunk = paged_chunk(held, even, most);
     CHECK(chunk >= 128 && chunk % 128 == 0);
-    CHECK(((long long)held + chunk - 1) / chunk <= std::max(most, 0));
+    CHECK(((long long)held + chunk - 1) / chunk <= paged_chunks(cap, even, most));
+    CHECK(paged_chunks(cap, even, most) >= 1 && paged_chunks(cap, even, most) <= most);
   }
   printf("index check ok\n");
   return 0;
