@@ -95,23 +95,34 @@ __host__ __device__ inline PagedTile paged_tile(const PagedSeq& q, int local) {
   return t;
 }
 
-// Positions per workgroup of the kernel for few rows, at a sequence whose cache holds `held`
-// positions: a share of `even` of them (as many as fill the device), but at least 128 and at most
-// kPagedMaxChunk (a long sequence among short ones is cut finer), unless that makes more than `most`.
+// How the kernel for few rows shares a sequence's positions among workgroups, in units of 128:
+// pieces of at most `unit` units, all of them alike, as long as there are no more than `most`.
 constexpr int kPagedMaxSplits = 64;
-constexpr int kPagedMaxChunk = 2048;
-__host__ __device__ inline int paged_chunk(int held, int even, int most) {
-  const int share = (held / even + 128) & ~127;  // more than held / even
-  const int least = (held / most + 128) & ~127;
-  const int chunk = share < kPagedMaxChunk ? share : kPagedMaxChunk;
-  return chunk > least ? chunk : least;
+constexpr int kPagedMaxUnit = 16;
+struct PagedPieces {
+  int count, size;  // pieces (at least 1), positions in each but the last
+};
+__host__ __device__ inline PagedPieces paged_pieces(int held, int unit, int most) {
+  const int units = (held + 127) >> 7;
+  int n = (units + unit - 1) / unit;
+  n = n < 1 ? 1 : n < most ? n : most;
+  const int each = units <= n ? 1 : (units + n - 1) / n;
+  return PagedPieces{n, each << 7};
 }
-// The most workgroups that share a sequence of up to `cap` positions.
-inline int paged_chunks(long long cap, int even, int most) {
-  long long n = cap / kPagedMaxChunk + 1;
-  if (n < even) n = even;
-  if (n > (cap + 127) / 128) n = (cap + 127) / 128;
-  return (int)(n < most ? n : most);
+// The unit for `total` units in all of a batch's sequences, `heads` key/value heads: as many
+// pieces as `want` workgroups.
+__host__ __device__ inline int paged_unit(long long total, int heads, int want) {
+  const long long u = (total * heads + want - 1) / want;
+  return u < 1 ? 1 : u < kPagedMaxUnit ? (int)u : kPagedMaxUnit;
+}
+// The most pieces of a sequence of up to `cap` positions, whatever the others' lengths: its own
+// length alone makes the unit at least units * heads / want.
+inline int paged_most_pieces(long long cap, int heads, int want, int most) {
+  const long long units = (cap + 127) >> 7;
+  long long n = units / kPagedMaxUnit + 1;
+  if (n < want / heads + 1) n = want / heads + 1;
+  if (n > units) n = units;
+  return (int)(n < 1 ? 1 : n < most ? n : most);
 }
 
 // ---- launches ----
@@ -141,7 +152,7 @@ struct PagedAttnParams {
   uint32_t* cnt;  // kPagedCounters arrival counters, zero between launches
   float* part;    // partial results of split sequences
   int splits;     // set by the launcher: the most workgroups that share a sequence's positions
-  int even, most; // set by the launcher: see paged_chunk
+  int want, most; // set by the launcher: workgroups that fill the device, and splits there is room for
   int min_rows;   // set by the launcher: sequences with more than min_rows rows per key/value head
   int max_rows;   // and at most max_rows are worked on
 };

@@ -101,12 +101,11 @@ __device__ __forceinline__ void load_query(const uint16_t* q, bool ok, float sca
   *mult = fmaxf(__builtin_amdgcn_ldexpf(scale, -e), kTiny);
 }
 
-// Exponent e with v < 2^e for the largest finite of non-negative scales, as an integer that
-// compares like it (0 for none).
-__device__ __forceinline__ uint32_t finite_bits(float v) {
-  const uint32_t b = __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu;
-  return b < 0x7F800000u ? b : 0u;
-}
+// Scales (none is negative) compare as their bits do, infinity above every number and NaN above it.
+constexpr uint32_t kInfBits = 0x7F800000u;
+__device__ __forceinline__ uint32_t bits_of(float v) { return __builtin_bit_cast(uint32_t, v); }
+__device__ __forceinline__ float as_float(uint32_t v) { return __builtin_bit_cast(float, v); }
+__device__ __forceinline__ uint32_t finite_bits(float v) { return bits_of(v) < kInfBits ? bits_of(v) : 0u; }
 
 __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
 
@@ -153,13 +152,24 @@ __device__ __forceinline__ void take_nonfinite(u32x4& v, const u32x4* sees, f32x
   __builtin_amdgcn_sched_barrier(0);  // one fragment at a time: this path is rare, registers are not
 }
 
-// Partials cross workgroups on different XCDs (separate L2s): accesses that go to memory, so that
-// no cache has to be written back or emptied.
-__device__ __forceinline__ void store_through(float* p, float v) {
-  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+// Partials cross workgroups on different XCDs (separate L2s): buffer accesses that go to memory (sc0
+// sc1), so that no cache has to be written back or emptied.  Word 3 is the gfx9 raw-buffer format.
+constexpr int kThrough = 1 | 16;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t partials(float* p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(p, (short)0, (int)bytes, 0x00020000);
 }
-__device__ __forceinline__ float load_through(const float* p) {
-  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+
+// v of the lane that the DPP control names, and op over the N (8 or 16) lanes that share a row.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, false));
+}
+template <int N, class F>
+__device__ __forceinline__ float over_lanes(float v, F op) {
+  v = op(v, dpp<0xB1>(v));
+  v = op(v, dpp<0x4E>(v));
+  v = op(v, dpp<0x141>(v));
+  return N == 16 ? op(v, dpp<0x140>(v)) : v;
 }
 
 // ---- few rows: one token of a sequence, or some ----
@@ -181,7 +191,8 @@ __global__ __launch_bounds__(64 * kFewWaves, U == 2 ? 2 : D == 128 ? 3 : 4) void
   constexpr int NL = 32 * D * ES / 1024;   // loads of 32 positions' keys (or values)
   constexpr int OS = D + 4;
   __shared__ __align__(16) float sacc[kFewWaves][R][OS];
-  __shared__ float sm[kFewWaves][R], sl[kFewWaves][R];
+  __shared__ float sm[kFewWaves][R], sl[kFewWaves][R];  // sm: then the wavefronts' weights
+  __shared__ float s_m[R], s_l[R];
   __shared__ int s_last;
 
   const int head = blockIdx.x % p.kv.heads, tile = blockIdx.x / p.kv.heads;
@@ -189,7 +200,8 @@ __global__ __launch_bounds__(64 * kFewWaves, U == 2 ? 2 : D == 128 ? 3 : 4) void
   const int col = lane & 15, g = lane >> 4;
   int local;
   PagedSeq q;
-  const int s = paged_find(p.seqs, p.kv.page_shift, tile, p.group, kFewShift<U>, 1, &local, &q);
+  int total = 0;
+  const int s = paged_find(p.seqs, p.kv.page_shift, tile, p.group, kFewShift<U>, 1, &local, &q, &total);
   if (s < 0) return;
   if ((long long)q.n * p.group <= p.min_rows || (long long)q.n * p.group > p.max_rows) return;
   const int row0 = local << kFewShift<U>;
@@ -198,7 +210,9 @@ __global__ __launch_bounds__(64 * kFewWaves, U == 2 ? 2 : D == 128 ? 3 : 4) void
   // a token at position t sees positions [0, t]; the tile's last one sees the most
   const int last = q.first + (row0 + rows - 1) / p.group;
   const int kend = max(min(q.held, last + 1), 0);
-  const int chunk = paged_chunk(q.held, p.even, p.most);
+  // (more than 64 sequences are work enough in large pieces)
+  const int unit = p.seqs.n_seq > 64 ? kPagedMaxUnit : paged_unit(total, p.kv.heads, p.want);
+  const int chunk = paged_pieces(q.held, unit, p.most).size;
   const int nchunk = max((kend + chunk - 1) / chunk, 1);
   const int c = blockIdx.y;
   if (c >= nchunk) return;
@@ -340,8 +354,13 @@ __global__ __launch_bounds__(64 * kFewWaves, U == 2 ? 2 : D == 128 ? 3 : 4) void
       if (FMT != KV_SAME) {
         uint32_t most = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          most = max(most, 16 * (e >> 2) + (e & 3) <= top ? finite_bits(vsc[e >> 2][e & 3]) : 0u);
+        for (int e = 0; e < 8; ++e) most = max(most, bits_of(vsc[e >> 2][e & 3]));
+        if (!whole || __ballot(most >= kInfBits)) {  // scales that no position has, or that are no numbers
+          most = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            most = max(most, 16 * (e >> 2) + (e & 3) <= top ? finite_bits(vsc[e >> 2][e & 3]) : 0u);
+        }
         e2 = max(ve, (int)(groups_umax(most) >> 23) - 126);
         const float to = __builtin_amdgcn_ldexpf(1.f, -e2);
 #pragma unroll
@@ -384,7 +403,11 @@ __global__ __launch_bounds__(64 * kFewWaves, U == 2 ? 2 : D == 128 ? 3 : 4) void
         if (FMT != KV_SAME) {
           al = __builtin_amdgcn_ldexpf(al, ve - e2);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] = vis[u] >> e & 1u ? w[e] * vs[e >> 2][e & 3] : 0.f;
+          for (int e = 0; e < 8; ++e) w[e] *= vs[e >> 2][e & 3];
+          if (!full) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = vis[u] >> e & 1u ? w[e] : 0.f;
+          }
         }
         if (__ballot(al != 1.f)) {
 #pragma unroll
@@ -450,55 +473,70 @@ __global__ __launch_bounds__(64 * kFewWaves, U == 2 ? 2 : D == 128 ? 3 : 4) void
   __syncthreads();
 
   // the wavefronts' sums, in order; one without a visible position has m = -inf and weight 0
-  auto joined = [&](int r, int d, float* M, float* L) {
-    float mx = sm[0][r];
+  const int t = threadIdx.x;
+  if (t < rows) {
+    float M = -INFINITY, L = 0.f;
 #pragma unroll
-    for (int i = 1; i < kFewWaves; ++i) mx = fmaxf(mx, sm[i][r]);
-    float o = 0.f, sum = 0.f;
+    for (int i = 0; i < kFewWaves; ++i) M = fmaxf(M, sm[i][t]);
 #pragma unroll
     for (int i = 0; i < kFewWaves; ++i) {
-      if (sm[i][r] == -INFINITY) {
-        if (mx == -INFINITY) sum += sl[i][r];
-      } else {
-        const float f = exp2_hw(sm[i][r] - mx);
-        o = fmaf(f, sacc[i][r][d], o);
-        sum = fmaf(f, sl[i][r], sum);
-      }
+      const bool none = sm[i][t] == -INFINITY;
+      const float f = none ? 0.f : exp2_hw(sm[i][t] - M);
+      // (without any, what counts is whether one of them saw a position: l is NaN then)
+      L += none ? (M == -INFINITY ? sl[i][t] : 0.f) : f * sl[i][t];
+      sm[i][t] = f;
     }
-    *M = mx;
-    *L = sum;
+    s_m[t] = M;
+    s_l[t] = L;
+  }
+  __syncthreads();
+  constexpr int kQuads = D / 4;  // 4 dimensions of a row to a thread
+  auto joined = [&](int r, int d) {
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kFewWaves; ++i) o += sm[i][r] * *(const f32x4*)&sacc[i][r][d];
     return o;
   };
-  auto out_at = [&](int r) {
+  auto row_of = [&](int r, int* token) {
     const int rr = row0 + r;
-    return (uint16_t*)p.out + (long long)(q.row + rr / p.group) * p.ldo + (head * p.group + rr % p.group) * D;
+    *token = q.row + rr / p.group;
+    return head * p.group + rr % p.group;
   };
-  auto part_at = [&](int r) {
-    const int rr = row0 + r;
-    return p.part + ((long long)(q.row + rr / p.group) * p.heads + head * p.group + rr % p.group) * p.splits * (D + 2);
+  auto finish = [&](int r, int d, f32x4 o, float L) {
+    int token;
+    const int qhead = row_of(r, &token);
+    if (L == 0.f) o = f32x4{0.f, 0.f, 0.f, 0.f};
+    else o = o / L;
+    *(u32x2*)((uint16_t*)p.out + (long long)token * p.ldo + qhead * D + d) =
+        u32x2{A::pack(o[0], o[1]), A::pack(o[2], o[3])};
   };
   if (nchunk == 1) {
-    for (int i = threadIdx.x; i < rows * D; i += 64 * kFewWaves) {
-      float M, L;
-      const float o = joined(i / D, i % D, &M, &L);
-      out_at(i / D)[i % D] = A::from_f32(L == 0.f ? 0.f : o / L);
+    for (int i = t; i < rows * kQuads; i += 64 * kFewWaves) {
+      const int r = i / kQuads, d = i % kQuads * 4;
+      finish(r, d, joined(r, d), s_l[r]);
     }
     return;
   }
-  for (int i = threadIdx.x; i < rows * D; i += 64 * kFewWaves) {
-    const int r = i / D, d = i % D;
-    float M, L;
-    const float o = joined(r, d, &M, &L);
-    float* at = part_at(r) + (long long)c * (D + 2);
-    store_through(at + 2 + d, o);
-    if (d == 0) {
-      store_through(at, M);
-      store_through(at + 1, L);
-    }
+  // partials: o [rows][splits][D], then (m, l) [rows][splits]
+  const uint32_t all_rows = (uint32_t)p.seqs.n_tokens * p.heads;
+  const uint32_t ml_at = all_rows * p.splits * D;
+  const auto part = partials(p.part, all_rows * p.splits * (D + 2) * 4);
+  auto slot = [&](int r, int k) {
+    int token;
+    const int qhead = row_of(r, &token);
+    return ((uint32_t)token * p.heads + qhead) * p.splits + k;
+  };
+  for (int i = t; i < rows * kQuads; i += 64 * kFewWaves) {
+    const int r = i / kQuads, d = i % kQuads * 4;
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, joined(r, d)), part, (slot(r, c) * D + d) * 4, 0,
+                                           kThrough);
   }
+  if (t < rows)
+    __builtin_amdgcn_raw_buffer_store_b64(u32x2{bits_of(s_m[t]), bits_of(s_l[t])}, part, (ml_at + slot(t, c) * 2) * 4, 0,
+                                          kThrough);
   __builtin_amdgcn_s_waitcnt(0);  // this thread's partials are in memory
   __syncthreads();
-  if (threadIdx.x == 0) {
+  if (t == 0) {
     uint32_t* cnt = p.cnt + blockIdx.x;
     const uint32_t prev = __hip_atomic_fetch_add(cnt, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     s_last = prev == (uint32_t)(nchunk - 1);
@@ -506,41 +544,54 @@ __global__ __launch_bounds__(64 * kFewWaves, U == 2 ? 2 : D == 128 ? 3 : 4) void
   }
   __syncthreads();
   if (!s_last) return;
-  // join the chunks, in order; weights of a row's chunks in LDS
+  // join the chunks, in order: N lanes share a row's (m, l), whose weights go to LDS, while the
+  // first partials are on their way
+  constexpr int N = 64 * kFewWaves / R, kPer = kPagedMaxSplits / N, kAhead = 8;
   float* weight = &sacc[0][0][0];  // [R][kPagedMaxSplits]
   static_assert(kPagedMaxSplits <= kFewWaves * OS, "chunk weights");
-  for (int i = threadIdx.x; i < rows * nchunk; i += 64 * kFewWaves) {
-    const int r = i / nchunk, k = i % nchunk;
-    weight[r * kPagedMaxSplits + k] = load_through(part_at(r) + (long long)k * (D + 2));
+  const int mr = t / N, mk = t % N;
+  u32x2 ml[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    ml[i] = mr < rows && mk + N * i < nchunk
+                ? __builtin_amdgcn_raw_buffer_load_b64(part, (ml_at + slot(mr, mk + N * i) * 2) * 4, 0, kThrough)
+                : u32x2{0xFF800000u, 0u};
+  u32x4 ahead[kAhead];
+  auto request = [&](int i, int k0) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (i < rows * kQuads && k0 + u < nchunk)
+        ahead[u] = __builtin_amdgcn_raw_buffer_load_b128(
+            part, (slot(i / kQuads, k0 + u) * D + i % kQuads * 4) * 4, 0, kThrough);
+  };
+  request(t, 0);
+  {
+    float M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) M = fmaxf(M, as_float(ml[i][0]));
+    M = over_lanes<N>(M, [](float x, float y) { return fmaxf(x, y); });
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const float m_i = as_float(ml[i][0]), l_i = as_float(ml[i][1]);
+      const bool none = m_i == -INFINITY;
+      const float f = none ? 0.f : exp2_hw(m_i - M);
+      L += none ? (M == -INFINITY ? l_i : 0.f) : f * l_i;
+      weight[mr * kPagedMaxSplits + mk + N * i] = f;
+    }
+    L = over_lanes<N>(L, [](float x, float y) { return x + y; });
+    if (mk == 0) s_l[mr] = L;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < rows * D; i += 64 * kFewWaves) {
-    const int r = i / D, d = i % D;
-    const float* at = part_at(r);
-    float M = -INFINITY, L = 0.f, o = 0.f;
-    for (int k = 0; k < nchunk; ++k) M = fmaxf(M, weight[r * kPagedMaxSplits + k]);
-    for (int k0 = 0; k0 < nchunk; k0 += 8) {
-      float ov[8], lv[8];
+  for (int i = t; i < rows * kQuads; i += 64 * kFewWaves) {
+    const int r = i / kQuads;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int k0 = 0; k0 < nchunk; k0 += kAhead) {
+      if (i != t || k0 > 0) request(i, k0);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const float* a = at + (long long)min(k0 + u, nchunk - 1) * (D + 2);
-        ov[u] = load_through(a + 2 + d);
-        lv[u] = load_through(a + 1);
-      }
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        if (k0 + u >= nchunk) continue;
-        const float mk = weight[r * kPagedMaxSplits + k0 + u];
-        if (mk == -INFINITY) {
-          if (M == -INFINITY) L += lv[u];
-        } else {
-          const float f = exp2_hw(mk - M);
-          L = fmaf(f, lv[u], L);
-          o = fmaf(f, ov[u], o);
-        }
-      }
+      for (int u = 0; u < kAhead; ++u)
+        if (k0 + u < nchunk) o += weight[r * kPagedMaxSplits + k0 + u] * __builtin_bit_cast(f32x4, ahead[u]);
     }
-    out_at(r)[d] = A::from_f32(L == 0.f ? 0.f : o / L);
+    finish(r, i % kQuads * 4, o, s_l[r]);
   }
 }
 
@@ -723,7 +774,14 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
       for (int t = 0; t < KT; ++t) {
         vs[t] = *(const f32x4*)&scales[b][kManyKeys + 16 * t + 4 * g];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) most = max(most, i <= top[t >> 1] - (jl + 16 * t) ? finite_bits(vs[t][i]) : 0u);
+        for (int i = 0; i < 4; ++i) most = max(most, bits_of(vs[t][i]));
+      }
+      if (!whole || __ballot(most >= kInfBits)) {
+        most = 0;
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) most = max(most, i <= top[t >> 1] - (jl + 16 * t) ? finite_bits(vs[t][i]) : 0u);
       }
       e2 = max(ve, (int)(groups_umax(most) >> 23) - 126);
       const float to = __builtin_amdgcn_ldexpf(1.f, -e2);
@@ -755,8 +813,11 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            w[4 * t + i] = vis[u] >> (4 * t + i) & 1u ? w[4 * t + i] * vs[t][i] : 0.f;
+          for (int i = 0; i < 4; ++i) w[4 * t + i] *= vs[t][i];
+        if (!full) {
+#pragma unroll
+          for (int i = 0; i < 4 * KT; ++i) w[i] = vis[u] >> i & 1u ? w[i] : 0.f;
+        }
       }
       if (__ballot(al != 1.f)) {
 #pragma unroll
@@ -985,18 +1046,17 @@ hipError_t many_a(const PagedAttnParams& p, const dim3& grid, hipStream_t st) {
 // the kernel for few rows when a batch needs both.
 constexpr int kFewRows = 32;
 
-// How the kernel for few rows deals a batch: kFewWorkgroups of even chunks fill the device (3 to 4
-// workgroups on each of 256 CUs), as far as the partials (kMaxPartials rows of all chunks) and the
-// counters go.
-constexpr int kFewWorkgroups = 1024;
+// How the kernel for few rows deals a batch: as many pieces as workgroups run at a time on 256
+// CUs (their registers allow 2 to 4 on each), as far as the partials (kMaxPartials rows of all
+// pieces) and the counters go.
 constexpr long long kMaxPartials = 1 << 18;
-void few_splits(PagedAttnParams* p, long long tiles) {
+void few_splits(PagedAttnParams* p, long long tiles, bool wide) {
   const long long cap = (long long)p->seqs.max_pages << p->kv.page_shift;
   const long long rows = (long long)p->seqs.n_tokens * p->heads;
   const long long room = tiles > kPagedCounters ? 1 : std::max<long long>(1, kMaxPartials / rows);
+  p->want = 256 * (p->kv.head_dim == 128 ? (wide ? 2 : 3) : (wide ? 3 : 4));
   p->most = (int)std::min<long long>(room, kPagedMaxSplits);
-  p->even = (int)std::min<long long>(std::max<long long>(1, (kFewWorkgroups + tiles / 2) / tiles), p->most);
-  p->splits = paged_chunks(cap, p->even, p->most);
+  p->splits = paged_most_pieces(cap, p->kv.heads, p->want, p->most);
 }
 
 // Workgroups that share a tile of the kernel for many rows.
@@ -1035,7 +1095,7 @@ hipError_t launch_paged_attention(PagedAttnParams p, double scale, void* ws, hip
   if (few) {
     const bool wide = longest > 16;
     const long long tiles = paged_tiles(b, p.group, wide ? kFewShift<2> : kFewShift<1>, 1) * p.kv.heads;
-    few_splits(&p, tiles);
+    few_splits(&p, tiles, wide);
     p.min_rows = 0;
     p.max_rows = many ? kFewRows : 0x7FFFFFFF;
     e = p.kv.dtype == 1 ? few_a<BF16>(p, wide, (unsigned)tiles, stream) : few_a<F16>(p, wide, (unsigned)tiles, stream);

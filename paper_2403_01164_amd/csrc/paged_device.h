@@ -85,11 +85,21 @@ __device__ __forceinline__ float groups_sum(float v) {
   return over_groups(v, [](float x, float y) { return x + y; });
 }
 
+// Sum over the wavefront, in every lane.
+__device__ __forceinline__ int wave_sum(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, false);   // lane ^ 1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, false);   // lane ^ 2
+  v += __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, false);  // mirrored half row
+  v += __builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, false);  // mirrored row of 16
+  return __builtin_amdgcn_readfirstlane((int)over_groups((uint32_t)v, [](uint32_t x, uint32_t y) { return x + y; }));
+}
+
 // Sequence of a tile (see paged_tile_base), the same in every lane of the wavefront: the last
 // one whose tiles begin at or before it, or -1; *local the tile's number within it, *seq its
-// rows and positions.  64 sequences at a time, in one round of loads.
+// rows and positions.  64 sequences at a time, in one round of loads.  *total: units of 128 positions
+// in all of the first 64 sequences that have new tokens.
 __device__ __forceinline__ int paged_find(const PagedSeqs& b, int page_shift, int tile, int unit, int shift, int extra,
-                                          int* local, PagedSeq* seq) {
+                                          int* local, PagedSeq* seq, int* total = nullptr) {
   const int lane = threadIdx.x & 63;
   int s = -1, start = 0, end = 0, len = 0;
   for (int i0 = 0; i0 < b.n_seq; i0 += 64) {
@@ -97,6 +107,10 @@ __device__ __forceinline__ int paged_find(const PagedSeqs& b, int page_shift, in
     const int st = load_i32(b.start + i), en = load_i32(b.start + i + 1), ln = load_i32(b.len + i);
     const bool before = i0 + lane < b.n_seq && paged_tile_base(st, i, b.n_tokens, unit, shift, extra) <= tile;
     const int c = __popcll(__ballot(before));
+    if (total && i0 == 0) {
+      const PagedSeq q = paged_seq(st, en, ln, b, page_shift);
+      *total = wave_sum(lane < b.n_seq && q.n > 0 ? (q.held + 127) >> 7 : 0);
+    }
     if (c > 0) {
       s = i0 + c - 1;
       start = __builtin_amdgcn_readlane(st, c - 1);

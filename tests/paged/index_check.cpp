@@ -115,14 +115,15 @@ int main() {
           CHECK(hits[start[s] + i] == (i < b.max_new && len[s] - n + i >= 0 ? 1 : 0));
         }
 
-    // chunks of a sequence: no more than its cap allows, whole steps, nothing left over
+    // pieces of a sequence: no more than its cap allows, whole steps, nothing left over or empty
     const int cap = pick(0, 1) ? pick(1, 100) * 32 : pick(1, 1 << 25) * 32;
-    const int most = pick(1, kPagedMaxSplits), even = pick(1, most);
+    const int most = pick(1, kPagedMaxSplits), heads = pick(1, 100), want = pick(1, 2000);
     const int held = std::min(cap, pick(0, 1) ? pick(0, 3000) : pick(0, 1 << 30));
-    const int chunk = paged_chunk(held, even, most);
-    CHECK(chunk >= 128 && chunk % 128 == 0);
-    CHECK(((long long)held + chunk - 1) / chunk <= paged_chunks(cap, even, most));
-    CHECK(paged_chunks(cap, even, most) >= 1 && paged_chunks(cap, even, most) <= most);
+    const long long others = pick(0, 1) ? 0 : pick(0, 1 << 24);
+    const PagedPieces s = paged_pieces(held, paged_unit(((held + 127) >> 7) + others, heads, want), most);
+    CHECK(s.size >= 128 && s.size % 128 == 0 && s.count >= 1);
+    CHECK((long long)s.count * s.size >= held);
+    CHECK(s.count <= paged_most_pieces(cap, heads, want, most) && paged_most_pieces(cap, heads, want, most) <= most);
   }
   printf("index check ok\n");
   return 0;
