@@ -95,8 +95,8 @@ __host__ __device__ inline PagedTile paged_tile(const PagedSeq& q, int local) {
   return t;
 }
 
-// How the kernel for few rows shares a sequence's positions among workgroups, in units of 128:
-// pieces of at most `unit` units, all of them alike, as long as there are no more than `most`.
+// The kernel for few rows shares a sequence's positions among workgroups, in units of 128: pieces
+// of at most `unit` units, all of them alike, as long as there are no more than `most`.
 constexpr int kPagedMaxSplits = 64;
 constexpr int kPagedMaxUnit = 16;
 struct PagedPieces {
@@ -109,20 +109,38 @@ __host__ __device__ inline PagedPieces paged_pieces(int held, int unit, int most
   const int each = units <= n ? 1 : (units + n - 1) / n;
   return PagedPieces{n, each << 7};
 }
-// The unit for `total` units in all of a batch's sequences, `heads` key/value heads: as many
-// pieces as `want` workgroups.
+// The unit for `total` units in all of a batch's tiles, `heads` key/value heads: as many pieces as
+// `want` workgroups, or as a few times that, so that the last of them end together.
 __host__ __device__ inline int paged_unit(long long total, int heads, int want) {
-  const long long u = (total * heads + want - 1) / want;
-  return u < 1 ? 1 : u < kPagedMaxUnit ? (int)u : kPagedMaxUnit;
+  const long long work = total * heads;
+  const long long rounds = (work + (long long)want * kPagedMaxUnit - 1) / ((long long)want * kPagedMaxUnit);
+  const long long u = (work + want * rounds - 1) / (want * (rounds < 1 ? 1 : rounds));
+  return u < 1 ? 1 : (int)u;
 }
-// The most pieces of a sequence of up to `cap` positions, whatever the others' lengths: its own
-// length alone makes the unit at least units * heads / want.
+// The most pieces of a sequence of up to `cap` positions, whatever the others' lengths: in one
+// round the unit is at least its own units * heads / want, in several at least half of
+// kPagedMaxUnit.
 inline int paged_most_pieces(long long cap, int heads, int want, int most) {
   const long long units = (cap + 127) >> 7;
-  long long n = units / kPagedMaxUnit + 1;
+  long long n = units / (kPagedMaxUnit / 2) + 1;
   if (n < want / heads + 1) n = want / heads + 1;
   if (n > units) n = units;
   return (int)(n < 1 ? 1 : n < most ? n : most);
+}
+// Tiles of a sequence with min_rows < rows <= max_rows, of `tile` rows.
+__host__ __device__ inline int paged_few_tiles(const PagedSeq& q, int group, int min_rows, int max_rows, int tile) {
+  const long long rows = (long long)q.n * group;
+  return rows <= min_rows || rows > max_rows ? 0 : (q.done * group + tile - 1) / tile;
+}
+// Items (tile, piece) of a batch of up to kPagedDense sequences are numbered without gaps, so that
+// workgroups without work do not come between the others (the device deals neighbouring workgroups
+// to its engines in turn); this many at most, tiles <= tiles_each for each sequence.
+constexpr int kPagedDense = 64;
+inline long long paged_most_items(long long cap, int n_seq, int tiles_each, int heads, int want, int most) {
+  const long long units = (cap + 127) >> 7;
+  const long long n = units * n_seq * tiles_each / kPagedMaxUnit + want / heads + 1 + (long long)n_seq * tiles_each;
+  const long long top = (long long)n_seq * tiles_each * paged_most_pieces(cap, heads, want, most);
+  return n < top ? n : top;
 }
 
 // ---- launches ----
@@ -153,6 +171,7 @@ struct PagedAttnParams {
   float* part;    // partial results of split sequences
   int splits;     // set by the launcher: the most workgroups that share a sequence's positions
   int want, most; // set by the launcher: workgroups that fill the device, and splits there is room for
+  int tiles_each; // set by the launcher: the most tiles of a sequence
   int min_rows;   // set by the launcher: sequences with more than min_rows rows per key/value head
   int max_rows;   // and at most max_rows are worked on
 };

@@ -183,6 +183,52 @@ constexpr int kFewWaves = 4;
 template <int U>
 constexpr int kFewShift = U == 2 ? 5 : 4;  // rows per tile: 16 U
 
+// A workgroup's work: rows [row0, row0 + 16 U) of sequence s and its chunk-th piece of positions.
+struct FewItem {
+  PagedSeq q;
+  int s, tile, chunk, size;  // size: positions of a piece
+  uint32_t counter;
+};
+
+// Item number w, the same in every lane of the wavefront; false: there is none.
+template <int U>
+__device__ __forceinline__ bool few_item(const PagedAttnParams& p, int w, FewItem* it) {
+  const PagedSeqs& b = p.seqs;
+  constexpr int R = 16 * U;
+  if (b.n_seq > kPagedDense) {  // work enough in large pieces; gaps and all, a piece of every tile at a time
+    const int tiles = (int)(((long long)b.n_tokens * p.group >> kFewShift<U>) + b.n_seq);
+    const int tile = w % tiles;
+    it->s = paged_find(b, p.kv.page_shift, tile, p.group, kFewShift<U>, 1, &it->tile, &it->q);
+    if (it->s < 0 || it->tile >= paged_few_tiles(it->q, p.group, p.min_rows, p.max_rows, R)) return false;
+    const PagedPieces piece = paged_pieces(it->q.held, kPagedMaxUnit, p.most);
+    it->chunk = w / tiles;
+    it->size = piece.size;
+    it->counter = (uint32_t)tile;
+    return it->chunk < piece.count;
+  }
+  const int lane = threadIdx.x & 63, i = min(lane, b.n_seq - 1);
+  const int st = load_i32(b.start + i);
+  const PagedSeq q = paged_seq(st, load_i32(b.start + i + 1), load_i32(b.len + i), b, p.kv.page_shift);
+  const int tiles = lane < b.n_seq ? paged_few_tiles(q, p.group, p.min_rows, p.max_rows, R) : 0;
+  const int unit = paged_unit(wave_sum(tiles * ((q.held + 127) >> 7)), p.kv.heads, p.want);
+  const PagedPieces piece = paged_pieces(q.held, unit, p.most);
+  const int items = tiles * piece.count;
+  const int upto = wave_scan(items);  // of this sequence and those before it
+  const uint64_t behind = __ballot(upto > w);
+  if (!behind) return false;
+  const int s = __builtin_ctzll(behind);
+  const int local = w - __builtin_amdgcn_readlane(upto - items, s), t = __builtin_amdgcn_readlane(tiles, s);
+  it->s = s;
+  it->q = PagedSeq{__builtin_amdgcn_readlane(q.row, s), __builtin_amdgcn_readlane(q.n, s),
+                   __builtin_amdgcn_readlane(q.done, s), __builtin_amdgcn_readlane(q.first, s),
+                   __builtin_amdgcn_readlane(q.held, s)};
+  it->tile = local % t;
+  it->chunk = local / t;
+  it->size = __builtin_amdgcn_readlane(piece.size, s);
+  it->counter = (uint32_t)(s * p.tiles_each + it->tile);
+  return true;
+}
+
 template <class A, int FMT, int D, int U>
 __global__ __launch_bounds__(64 * kFewWaves, U == 2 ? 2 : D == 128 ? 3 : 4) void paged_few_kernel(PagedAttnParams p) {
   typedef typename Compute<A, FMT>::type T;
@@ -195,28 +241,24 @@ __global__ __launch_bounds__(64 * kFewWaves, U == 2 ? 2 : D == 128 ? 3 : 4) void
   __shared__ float s_m[R], s_l[R];
   __shared__ int s_last;
 
-  const int head = blockIdx.x % p.kv.heads, tile = blockIdx.x / p.kv.heads;
+  const int head = blockIdx.x % p.kv.heads;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g = lane >> 4;
-  int local;
-  PagedSeq q;
-  int total = 0;
-  const int s = paged_find(p.seqs, p.kv.page_shift, tile, p.group, kFewShift<U>, 1, &local, &q, &total);
-  if (s < 0) return;
-  if ((long long)q.n * p.group <= p.min_rows || (long long)q.n * p.group > p.max_rows) return;
-  const int row0 = local << kFewShift<U>;
+  FewItem it;
+  // a lone sequence's first 64 pages need not wait for its length
+  const bool lone = p.seqs.n_seq == 1;
+  const int first_pages = lone && lane < p.seqs.max_pages ? load_i32(p.seqs.table + lane) : -1;
+  if (!few_item<U>(p, blockIdx.x / p.kv.heads, &it)) return;
+  const PagedSeq& q = it.q;
+  const int s = it.s, c = it.chunk;
+  const int row0 = it.tile << kFewShift<U>;
   const int rows = min(q.done * p.group - row0, R);  // of this tile
-  if (rows <= 0) return;
   // a token at position t sees positions [0, t]; the tile's last one sees the most
   const int last = q.first + (row0 + rows - 1) / p.group;
   const int kend = max(min(q.held, last + 1), 0);
-  // (more than 64 sequences are work enough in large pieces)
-  const int unit = p.seqs.n_seq > 64 ? kPagedMaxUnit : paged_unit(total, p.kv.heads, p.want);
-  const int chunk = paged_pieces(q.held, unit, p.most).size;
-  const int nchunk = max((kend + chunk - 1) / chunk, 1);
-  const int c = blockIdx.y;
+  const int nchunk = max((kend + it.size - 1) / it.size, 1);
   if (c >= nchunk) return;
-  const int j0 = c * chunk, j1 = min(j0 + chunk, kend);
+  const int j0 = c * it.size, j1 = min(j0 + it.size, kend);
   const int nsteps = (max(j1 - j0, 0) + 31) >> 5;
 
   const int minpos = q.first + row0 / p.group;  // the least a row of the tile sees to
@@ -249,7 +291,12 @@ __global__ __launch_bounds__(64 * kFewWaves, U == 2 ? 2 : D == 128 ? 3 : 4) void
   int pages = -1;
   auto look_up = [&](int n0) {
     const int j = j0 + 32 * (wave + kFewWaves * (n0 + lane));
-    pages = j < j1 ? paged_page(p.seqs, p.kv, s, j) : -1;
+    if (lone && (j1 - 1) >> p.kv.page_shift < 64) {
+      const int entry = paged_entry(p.kv, __shfl(first_pages, (j >> p.kv.page_shift) & 63));
+      pages = j < j1 ? entry : -1;
+    } else {
+      pages = j < j1 ? paged_page(p.seqs, p.kv, s, j) : -1;
+    }
   };
   auto load_keys = [&](int page, int j) {
     const char* rec = base + max(page, 0) * page_bytes;
@@ -537,7 +584,7 @@ __global__ __launch_bounds__(64 * kFewWaves, U == 2 ? 2 : D == 128 ? 3 : 4) void
   __builtin_amdgcn_s_waitcnt(0);  // this thread's partials are in memory
   __syncthreads();
   if (t == 0) {
-    uint32_t* cnt = p.cnt + blockIdx.x;
+    uint32_t* cnt = p.cnt + it.counter * p.kv.heads + head;
     const uint32_t prev = __hip_atomic_fetch_add(cnt, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     s_last = prev == (uint32_t)(nchunk - 1);
     if (s_last) __hip_atomic_store(cnt, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -1005,21 +1052,21 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p) {
 }
 
 template <class A, int FMT, int D>
-hipError_t few_t(PagedAttnParams p, bool wide, unsigned tiles, hipStream_t st) {
-  const dim3 grid(tiles, p.splits);
+hipError_t few_t(PagedAttnParams p, bool wide, unsigned items, hipStream_t st) {
+  const dim3 grid(items);
   if (wide) hipLaunchKernelGGL((paged_few_kernel<A, FMT, D, 2>), grid, dim3(64 * kFewWaves), 0, st, p);
   else hipLaunchKernelGGL((paged_few_kernel<A, FMT, D, 1>), grid, dim3(64 * kFewWaves), 0, st, p);
   return hipGetLastError();
 }
 
 template <class A>
-hipError_t few_a(const PagedAttnParams& p, bool wide, unsigned tiles, hipStream_t st) {
+hipError_t few_a(const PagedAttnParams& p, bool wide, unsigned items, hipStream_t st) {
   const bool d128 = p.kv.head_dim == 128;
   switch (p.kv.format) {
-    case KV_SAME: return d128 ? few_t<A, KV_SAME, 128>(p, wide, tiles, st) : few_t<A, KV_SAME, 64>(p, wide, tiles, st);
-    case KV_I8: return d128 ? few_t<A, KV_I8, 128>(p, wide, tiles, st) : few_t<A, KV_I8, 64>(p, wide, tiles, st);
+    case KV_SAME: return d128 ? few_t<A, KV_SAME, 128>(p, wide, items, st) : few_t<A, KV_SAME, 64>(p, wide, items, st);
+    case KV_I8: return d128 ? few_t<A, KV_I8, 128>(p, wide, items, st) : few_t<A, KV_I8, 64>(p, wide, items, st);
   }
-  return d128 ? few_t<A, KV_E4M3, 128>(p, wide, tiles, st) : few_t<A, KV_E4M3, 64>(p, wide, tiles, st);
+  return d128 ? few_t<A, KV_E4M3, 128>(p, wide, items, st) : few_t<A, KV_E4M3, 64>(p, wide, items, st);
 }
 
 template <class A, int FMT, int D>
@@ -1048,15 +1095,23 @@ constexpr int kFewRows = 32;
 
 // How the kernel for few rows deals a batch: as many pieces as workgroups run at a time on 256
 // CUs (their registers allow 2 to 4 on each), as far as the partials (kMaxPartials rows of all
-// pieces) and the counters go.
+// pieces) and the counters go.  Returns the number of workgroups.
 constexpr long long kMaxPartials = 1 << 18;
-void few_splits(PagedAttnParams* p, long long tiles, bool wide) {
+long long few_splits(PagedAttnParams* p, long long tiles, bool wide, long long rows_each) {
   const long long cap = (long long)p->seqs.max_pages << p->kv.page_shift;
   const long long rows = (long long)p->seqs.n_tokens * p->heads;
-  const long long room = tiles > kPagedCounters ? 1 : std::max<long long>(1, kMaxPartials / rows);
+  const int heads = p->kv.heads, n_seq = p->seqs.n_seq;
+  p->tiles_each = (int)((rows_each + (wide ? 31 : 15)) / (wide ? 32 : 16));
+  const long long counters = n_seq > kPagedDense ? tiles : (long long)n_seq * p->tiles_each * heads;
+  const long long room = counters > kPagedCounters ? 1 : std::max<long long>(1, kMaxPartials / rows);
   p->want = 256 * (p->kv.head_dim == 128 ? (wide ? 2 : 3) : (wide ? 3 : 4));
   p->most = (int)std::min<long long>(room, kPagedMaxSplits);
-  p->splits = paged_most_pieces(cap, p->kv.heads, p->want, p->most);
+  p->splits = paged_most_pieces(cap, heads, p->want, p->most);
+  if (n_seq > kPagedDense) {
+    p->splits = (int)std::min<long long>(p->splits, ((cap + 127) / 128 + kPagedMaxUnit - 1) / kPagedMaxUnit);
+    return tiles * p->splits;
+  }
+  return heads * paged_most_items(cap, n_seq, p->tiles_each, heads, p->want, p->most);
 }
 
 // Workgroups that share a tile of the kernel for many rows.
@@ -1095,10 +1150,10 @@ hipError_t launch_paged_attention(PagedAttnParams p, double scale, void* ws, hip
   if (few) {
     const bool wide = longest > 16;
     const long long tiles = paged_tiles(b, p.group, wide ? kFewShift<2> : kFewShift<1>, 1) * p.kv.heads;
-    few_splits(&p, tiles, wide);
+    const unsigned items = (unsigned)few_splits(&p, tiles, wide, std::min(longest, (long long)kFewRows));
     p.min_rows = 0;
     p.max_rows = many ? kFewRows : 0x7FFFFFFF;
-    e = p.kv.dtype == 1 ? few_a<BF16>(p, wide, (unsigned)tiles, stream) : few_a<F16>(p, wide, (unsigned)tiles, stream);
+    e = p.kv.dtype == 1 ? few_a<BF16>(p, wide, items, stream) : few_a<F16>(p, wide, items, stream);
   }
   if (e == hipSuccess && many) {
     p.splits = many_splits(p.kv, b, p.heads);

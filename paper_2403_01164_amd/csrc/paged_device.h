@@ -94,12 +94,22 @@ __device__ __forceinline__ int wave_sum(int v) {
   return __builtin_amdgcn_readfirstlane((int)over_groups((uint32_t)v, [](uint32_t x, uint32_t y) { return x + y; }));
 }
 
+// Sum over the lanes up to this one.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // from 1, 2, 4 and 8 lanes below, within 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // lane 15 of the row below, to rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // lane 31, to rows 2 and 3
+  return v;
+}
+
 // Sequence of a tile (see paged_tile_base), the same in every lane of the wavefront: the last
 // one whose tiles begin at or before it, or -1; *local the tile's number within it, *seq its
-// rows and positions.  64 sequences at a time, in one round of loads.  *total: units of 128 positions
-// in all of the first 64 sequences that have new tokens.
+// rows and positions.  64 sequences at a time, in one round of loads.
 __device__ __forceinline__ int paged_find(const PagedSeqs& b, int page_shift, int tile, int unit, int shift, int extra,
-                                          int* local, PagedSeq* seq, int* total = nullptr) {
+                                          int* local, PagedSeq* seq) {
   const int lane = threadIdx.x & 63;
   int s = -1, start = 0, end = 0, len = 0;
   for (int i0 = 0; i0 < b.n_seq; i0 += 64) {
@@ -107,10 +117,6 @@ __device__ __forceinline__ int paged_find(const PagedSeqs& b, int page_shift, in
     const int st = load_i32(b.start + i), en = load_i32(b.start + i + 1), ln = load_i32(b.len + i);
     const bool before = i0 + lane < b.n_seq && paged_tile_base(st, i, b.n_tokens, unit, shift, extra) <= tile;
     const int c = __popcll(__ballot(before));
-    if (total && i0 == 0) {
-      const PagedSeq q = paged_seq(st, en, ln, b, page_shift);
-      *total = wave_sum(lane < b.n_seq && q.n > 0 ? (q.held + 127) >> 7 : 0);
-    }
     if (c > 0) {
       s = i0 + c - 1;
       start = __builtin_amdgcn_readlane(st, c - 1);
@@ -126,10 +132,10 @@ __device__ __forceinline__ int paged_find(const PagedSeqs& b, int page_shift, in
   return s;
 }
 
-// Page of position j (j < held) of sequence s; -1 where the table names none.
+// A table entry, -1 where it names no page, and the page of position j (j < held) of sequence s.
+__device__ __forceinline__ int paged_entry(const PagedCache& kv, int p) { return p >= 0 && p < kv.n_pages ? p : -1; }
 __device__ __forceinline__ int paged_page(const PagedSeqs& b, const PagedCache& kv, int s, int j) {
-  const int p = load_i32(b.table + (size_t)s * b.max_pages + (j >> kv.page_shift));
-  return p >= 0 && p < kv.n_pages ? p : -1;
+  return paged_entry(kv, load_i32(b.table + (size_t)s * b.max_pages + (j >> kv.page_shift)));
 }
 
 }  // namespace

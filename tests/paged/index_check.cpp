@@ -124,6 +124,28 @@ int main() {
     CHECK(s.size >= 128 && s.size % 128 == 0 && s.count >= 1);
     CHECK((long long)s.count * s.size >= held);
     CHECK(s.count <= paged_most_pieces(cap, heads, want, most) && paged_most_pieces(cap, heads, want, most) <= most);
+
+    // items (tile, piece) of a batch without gaps: no more than the launch has workgroups for
+    if (b.n_seq > kPagedDense || b.n_tokens == 0) continue;
+    const int group = pick(1, 4), R = pick(0, 1) ? 16 : 32, cap_b = b.max_pages * page;
+    const bool limited = pick(0, 1);  // the kernel for many rows takes the others
+    const int max_rows = limited ? 32 : 0x7FFFFFFF;
+    const long long longest = (long long)std::min(b.max_new, b.n_tokens) * group;
+    const int each = (int)((std::min<long long>(longest, limited ? 32 : longest) + R - 1) / R);
+    long long total = 0, items = 0;
+    for (int pass = 0; pass < 2; ++pass) {
+      const int unit = paged_unit(total, heads, want);
+      for (int i = 0; i < b.n_seq; ++i) {
+        const PagedSeq q = paged_seq(b.start[i], b.start[i + 1], b.len[i], b, shift);
+        const int tiles = paged_few_tiles(q, group, 0, max_rows, R);
+        CHECK(tiles <= each);
+        if (pass == 0) total += (long long)tiles * ((q.held + 127) >> 7);
+        else items += (long long)tiles * paged_pieces(q.held, unit, most).count;
+        if (pass == 1 && tiles)
+          CHECK(paged_pieces(q.held, unit, most).count <= paged_most_pieces(cap_b, heads, want, most));
+      }
+    }
+    CHECK(items <= paged_most_items(cap_b, b.n_seq, each, heads, want, most));
   }
   printf("index check ok\n");
   return 0;
