@@ -107,6 +107,10 @@ __device__ __forceinline__ uint32_t bits_of(float v) { return __builtin_bit_cast
 __device__ __forceinline__ float as_float(uint32_t v) { return __builtin_bit_cast(float, v); }
 __device__ __forceinline__ uint32_t finite_bits(float v) { return bits_of(v) < kInfBits ? bits_of(v) : 0u; }
 
+// The larger of two numbers in one instruction: fmaxf would first make each one canonical, which
+// the products' sums are not known to be.
+__device__ __forceinline__ float max_of(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); }
+
 __device__ __forceinline__ float exp2_hw(float v) { return __builtin_amdgcn_exp2f(v); }
 
 // Infinities and NaNs in values.  A product gives 0 * infinity = NaN to queries that do not see a
@@ -648,8 +652,10 @@ __global__ __launch_bounds__(64 * kFewWaves, U == 2 ? 2 : D == 128 ? 3 : 4) void
 // rows each; 64 positions at a time go through LDS, one buffer being filled while the other is
 // multiplied: 16-bit pages by loads that write to LDS themselves (the pages' order is the operands'
 // order already), 8-bit ones through registers, where they become fp16.  Every operand read from
-// LDS feeds two products.  When there are few tiles, several workgroups share a tile's positions
-// and a second kernel joins their partials.
+// LDS feeds two products.  The scores of the next step are computed beside the weights of this one,
+// so that matrix cores and vector units have work at the same time, and a step has one barrier.
+// When there are few tiles, several workgroups share a tile's positions and a second kernel joins
+// their partials.
 constexpr int kManyWaves = 4;
 constexpr int kManyShift = 7;  // rows per tile: 128
 constexpr int kManyKeys = 64;  // positions at a time
@@ -672,8 +678,8 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
   constexpr int KT = kManyKeys / 16;             // key tiles of a step
   constexpr int kSide = kManyKeys * D * 2;       // bytes of a step's keys (or values) in LDS
   constexpr int NL = kManyKeys * D * ES * 2 / 1024 / kManyWaves;  // loads of a step, per wavefront
-  __shared__ __align__(16) char buf0[2 * kSide], buf1[2 * kSide];
-  __shared__ float scales[2][FMT == KV_SAME ? 1 : 2 * kManyKeys];
+  __shared__ __align__(16) char keys0[kSide], keys1[kSide], values0[kSide], values1[kSide];
+  __shared__ float scales[2][FMT == KV_SAME ? 1 : 2 * kManyKeys];  // of keys, then of values, by step % 2
   __shared__ int s_odd;
 
   const int head = blockIdx.x % p.kv.heads, tile = blockIdx.x / p.kv.heads;
@@ -720,30 +726,33 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
   const long long page_bytes = p.kv.record * p.kv.heads;
 
   f32x4 O[U][DT];
+  f32x4 lsum[U];  // 16-bit pages: the sums of weights come from a product with ones, alike in all elements
   float m[U], l[U];
   uint32_t seen[U];
   int ve;
   int pages = -1;  // lane i: the page of the i-th 32 positions from the last look-up on
   u32x4 raw[NL];   // 8-bit pages on their way to LDS
   float raw_scale = 0.f;
+  struct Halves {
+    int a, b;  // pages of a step's 32-position halves (-1: none)
+  };
+  const int half = wave & 1, side = wave >> 1;  // a wavefront brings one half's keys (0) or values (1)
 
-  // a step's 32-position halves: their pages (-1: none)
-  auto half_pages = [&](int step, int* a, int* b) {
+  // of a step, in order of steps
+  auto halves = [&](int step) {
     const int i = 2 * (step & 31);
     if (i == 0) {
       const int j = j0 + kManyKeys * step + 32 * lane;
       pages = j < j1 ? paged_page(p.seqs, p.kv, s, j) : -1;
     }
-    *a = __builtin_amdgcn_readlane(pages, i);
-    *b = __builtin_amdgcn_readlane(pages, i + 1);
+    return Halves{__builtin_amdgcn_readlane(pages, i), __builtin_amdgcn_readlane(pages, i + 1)};
   };
-  auto issue = [&](char* buf, int step, int pa, int pb) {
-    const int half = wave & 1, side = wave >> 1;  // a wavefront brings one half's keys or values
+  auto issue = [&](char* keys, char* values, int step, Halves pg) {
     const int j = j0 + kManyKeys * step + 32 * half;
-    const char* rec = base + max(half ? pb : pa, 0) * page_bytes;
+    const char* rec = base + max(half ? pg.b : pg.a, 0) * page_bytes;
     const char* src = rec + (side * P + (j & pmask)) * D * ES + lane * 16;
     if (FMT == KV_SAME) {
-      char* dst = buf + side * kSide + half * (kSide / 2);
+      char* dst = (side ? values : keys) + half * (kSide / 2);
 #pragma unroll
       for (int i = 0; i < NL; ++i)
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(src + i * 1024),
@@ -754,45 +763,59 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
       if (lane < 32) raw_scale = ((const float*)(rec + 2 * P * D))[side * P + (j & pmask) + lane];
     }
   };
-  auto commit = [&](char* buf, int b) {
+  auto commit = [&](char* keys, char* values, int step) {
     if (FMT != KV_SAME) {
-      const int half = wave & 1, side = wave >> 1;
-      char* dst = buf + side * kSide + half * (kSide / 2) + lane * 16;
+      char* dst = (side ? values : keys) + half * (kSide / 2) + lane * 16;
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         *(u32x4*)(dst + 2 * i * 1024) = codes_f16<FMT>(raw[i][0], raw[i][1]);
         *(u32x4*)(dst + (2 * i + 1) * 1024) = codes_f16<FMT>(raw[i][2], raw[i][3]);
       }
-      if (lane < 32) scales[b][side * kManyKeys + 32 * half + lane] = raw_scale;
+      if (lane < 32) scales[step & 1][side * kManyKeys + 32 * half + lane] = raw_scale;
     }
   };
-  auto compute = [&](const char* buf, int b, int step, int pa, int pb, auto again) {
-    constexpr bool careful = decltype(again)::value;
-    const int jb = j0 + kManyKeys * step;
-    if (jb > wmax) return;
-    const char* kb = buf + lane * 16;
-    const char* vb = buf + kSide + lane * 16;
-    f32x4 sc[KT][U];
+  auto score = [&](const char* keys, int step, f32x4(&sc)[KT][U]) {
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
 #pragma unroll
       for (int u = 0; u < U; ++u) sc[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int k = 0; k < KK; ++k) {
-        const u32x4 kf = *(const u32x4*)(kb + (t * KK + k) * 1024);
+        const u32x4 kf = *(const u32x4*)(keys + lane * 16 + (t * KK + k) * 1024);
 #pragma unroll
         for (int u = 0; u < U; ++u) sc[t][u] = T::mfma(kf, qf[u][k], sc[t][u]);
       }
       if (FMT != KV_SAME) {
-        const f32x4 ks = *(const f32x4*)&scales[b][16 * t + 4 * g];
+        const f32x4 ks = *(const f32x4*)&scales[step & 1][16 * t + 4 * g];
 #pragma unroll
         for (int u = 0; u < U; ++u) sc[t][u] *= ks;
       }
     }
-    const bool whole = pa >= 0 && pb >= 0 && jb + kManyKeys <= q.held;
+  };
+  // what lies behind a sequence's end was never written and may be anything: zeros for its values
+  auto blank = [&](char* values, int step, Halves pg) {
+    for (int i = threadIdx.x; i < kSide / 16; i += 64 * kManyWaves) {
+      const int h = i >= kSide / 32, vg = (i & 63) >> 4;
+      const int top = ((h ? pg.b : pg.a) >= 0 ? q.held - 1 : -1) - (j0 + kManyKeys * step + 32 * h + 4 * vg);
+      u32x4* at = (u32x4*)values + i;
+      u32x4 v = *at;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int to = top - (16 * (w >> 1) + 2 * (w & 1));
+        v[w] &= (to >= 0 ? 0xFFFFu : 0u) | (to >= 1 ? 0xFFFF0000u : 0u);
+      }
+      *at = v;
+    }
+  };
+  // one step: sc are its scores, and the next step's (of next_keys) afterwards
+  auto compute = [&](const char* next_keys, const char* values, int step, Halves pg, f32x4(&sc)[KT][U], auto again) {
+    constexpr bool careful = decltype(again)::value;
+    const int jb = j0 + kManyKeys * step;
+    if (jb > wmax) return;
+    const bool whole = pg.a >= 0 && pg.b >= 0 && jb + kManyKeys <= q.held;
     const bool full = whole && jb + kManyKeys - 1 <= wmin;
     // last position of either half that is in the cache
-    const int top[2] = {pa >= 0 ? q.held - 1 : -1, pb >= 0 ? q.held - 1 : -1};
+    const int top[2] = {pg.a >= 0 ? q.held - 1 : -1, pg.b >= 0 ? q.held - 1 : -1};
     const int jl = jb + 4 * g;  // element i of key tile t is position jl + 16 t + i
     uint32_t vis[U];
 #pragma unroll
@@ -819,7 +842,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
       uint32_t most = 0;
 #pragma unroll
       for (int t = 0; t < KT; ++t) {
-        vs[t] = *(const f32x4*)&scales[b][kManyKeys + 16 * t + 4 * g];
+        vs[t] = *(const f32x4*)&scales[step & 1][kManyKeys + 16 * t + 4 * g];
 #pragma unroll
         for (int i = 0; i < 4; ++i) most = max(most, bits_of(vs[t][i]));
       }
@@ -835,56 +858,62 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
 #pragma unroll
       for (int t = 0; t < KT; ++t) vs[t] *= to;
     }
+    float ms[U], al[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float mx = sc[0][u][0];
+#pragma unroll
+      for (int e = 1; e < 4 * KT; ++e) mx = max_of(mx, sc[e >> 2][u][e & 3]);
+      mx = fmaxf(m[u], groups_max(mx) * mult[u]);
+      ms[u] = mx == -INFINITY ? 0.f : mx;
+      al[u] = exp2_hw(m[u] - ms[u]);
+      m[u] = mx;
+      l[u] *= al[u];
+      lsum[u] *= al[u];
+      if (FMT != KV_SAME) al[u] = __builtin_amdgcn_ldexpf(al[u], ve - e2);
+      if (__ballot(al[u] != 1.f)) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) O[u][dt] *= al[u];
+      }
+    }
+    ve = e2;
+    f32x4 next[KT][U];
+    score(next_keys, step + 1, next);
+    // weights, rounded to 16 bits once: their errors average out over the positions
     u32x4 pf[U][KT / 2];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float mx = -INFINITY;
-#pragma unroll
-      for (int t = 0; t < KT; ++t)
-        mx = fmaxf(mx, fmaxf(fmaxf(sc[t][u][0], sc[t][u][1]), fmaxf(sc[t][u][2], sc[t][u][3])));
-      mx = fmaxf(m[u], groups_max(mx) * mult[u]);
-      const float ms = mx == -INFINITY ? 0.f : mx;
-      float al = exp2_hw(m[u] - ms), sum = 0.f;
-      m[u] = mx;
       float w[KT * 4];
 #pragma unroll
-      for (int t = 0; t < KT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          w[4 * t + i] = exp2_hw(fmaf(sc[t][u][i], mult[u], -ms));
-          sum += w[4 * t + i];
-        }
-      l[u] = fmaf(l[u], al, sum);
+      for (int e = 0; e < 4 * KT; ++e) w[e] = exp2_hw(fmaf(sc[e >> 2][u][e & 3], mult[u], -ms[u]));
       if (FMT != KV_SAME) {
-        al = __builtin_amdgcn_ldexpf(al, ve - e2);
 #pragma unroll
-        for (int t = 0; t < KT; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) w[4 * t + i] *= vs[t][i];
+        for (int e = 0; e < 4 * KT; ++e) {
+          l[u] += w[e];
+          w[e] *= vs[e >> 2][e & 3];
+        }
         if (!full) {
 #pragma unroll
-          for (int i = 0; i < 4 * KT; ++i) w[i] = vis[u] >> i & 1u ? w[i] : 0.f;
+          for (int e = 0; e < 4 * KT; ++e) w[e] = vis[u] >> e & 1u ? w[e] : 0.f;
         }
       }
-      if (__ballot(al != 1.f)) {
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) O[u][dt] *= al;
-      }
-      // weights rounded to 16 bits once: their errors average out over the positions
 #pragma unroll
       for (int h = 0; h < KT / 2; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i) pf[u][h][i] = T::pack(w[8 * h + 2 * i], w[8 * h + 2 * i + 1]);
     }
-    ve = e2;
+    const uint32_t one = (uint32_t)T::from_f32(1.f) * 0x00010001u;
 #pragma unroll
     for (int h = 0; h < KT / 2; ++h) {
       u32x4 sees[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) sees[u] = seen_keys<T>(vis[u] >> (8 * h));
+      for (int u = 0; u < U; ++u) {
+        sees[u] = seen_keys<T>(vis[u] >> (8 * h));
+        if (FMT == KV_SAME) lsum[u] = T::mfma(u32x4{one, one, one, one}, pf[u][h], lsum[u]);
+      }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
-        u32x4 vf = *(const u32x4*)(vb + h * (kSide / 2) + dt * 1024);
+        u32x4 vf = *(const u32x4*)(values + lane * 16 + h * (kSide / 2) + dt * 1024);
         if (careful) {
           f32x4* const o[2] = {&O[0][dt], &O[1][dt]};
           take_nonfinite<T, U>(vf, sees, o);
@@ -893,21 +922,10 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
         for (int u = 0; u < U; ++u) O[u][dt] = T::mfma(vf, pf[u][h], O[u][dt]);
       }
     }
-  };
-  // what lies behind a sequence's end was never written and may be anything: zeros for its values
-  auto blank = [&](char* buf, int step, int pa, int pb) {
-    for (int i = threadIdx.x; i < kSide / 16; i += 64 * kManyWaves) {
-      const int half = i >= kSide / 32, vg = (i & 63) >> 4;
-      const int top = ((half ? pb : pa) >= 0 ? q.held - 1 : -1) - (j0 + kManyKeys * step + 32 * half + 4 * vg);
-      u32x4* at = (u32x4*)(buf + kSide) + i;
-      u32x4 v = *at;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int to = top - (16 * (w >> 1) + 2 * (w & 1));
-        v[w] &= (to >= 0 ? 0xFFFFu : 0u) | (to >= 1 ? 0xFFFF0000u : 0u);
-      }
-      *at = v;
-    }
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int u = 0; u < U; ++u) sc[t][u] = next[t][u];
   };
 
   auto walk = [&](auto again) {
@@ -916,39 +934,46 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
     for (int u = 0; u < U; ++u) {
       m[u] = -INFINITY;
       l[u] = 0.f;
+      lsum[u] = f32x4{0.f, 0.f, 0.f, 0.f};
       seen[u] = 0;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) O[u][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    int pa = -1, pb = -1;
-    if (nsteps > 0) {
-      half_pages(0, &pa, &pb);
-      issue(buf0, 0, pa, pb);
-      commit(buf0, 0);
-    }
-    // one barrier a step: behind it the step's buffer is filled and nobody reads the other one
-    auto turn = [&](char* now, char* other, int b, int step) {
+    if (nsteps == 0) return;
+    // before step 0: its keys and values are in LDS, its scores known, the next keys on their way
+    Halves pg0 = halves(0), pg1{-1, -1};
+    issue(keys0, values0, 0, pg0);
+    commit(keys0, values0, 0);
+    if (nsteps > 1) pg1 = halves(1);
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (nsteps > 1 && side == 0) issue(keys1, values1, 1, pg1);
+    f32x4 sc[KT][U];
+    score(keys0, 0, sc);
+    if (nsteps > 1 && side == 0) commit(keys1, values1, 1);
+    // a step: behind its barrier its values and the next keys are in LDS, and nobody reads the
+    // other two buffers, which take the keys after those and the next values
+    auto turn = [&](char* next_keys, char* keys, char* values, char* next_values, int step) {
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();
-      int na = -1, nb = -1;
-      const bool more = step + 1 < nsteps;
-      if (more) {
-        half_pages(step + 1, &na, &nb);
-        issue(other, step + 1, na, nb);
-      }
-      if (pa < 0 || pb < 0 || j0 + kManyKeys * (step + 1) > q.held) {
-        blank(now, step, pa, pb);
+      Halves pg2{-1, -1};
+      if (step + 2 < nsteps) pg2 = halves(step + 2);
+      const bool more = step + 2 - side < nsteps;
+      if (more) issue(keys, next_values, step + 2 - side, side ? pg1 : pg2);
+      if (pg0.a < 0 || pg0.b < 0 || j0 + kManyKeys * (step + 1) > q.held) {
+        blank(values, step, pg0);
         __syncthreads();
       }
-      compute(now, b, step, pa, pb, again);
-      if (more) commit(other, 1 - b);
-      pa = na;
-      pb = nb;
+      compute(next_keys, values, step, pg0, sc, again);
+      if (more) commit(keys, next_values, step + 2 - side);
+      pg0 = pg1;
+      pg1 = pg2;
     };
     for (int step = 0; step < nsteps; step += 2) {
-      turn(buf0, buf1, 0, step);
-      if (step + 1 < nsteps) turn(buf1, buf0, 1, step + 1);
+      turn(keys1, keys0, values0, values1, step);
+      if (step + 1 < nsteps) turn(keys0, keys1, values1, values0, step + 1);
     }
+    __syncthreads();
   };
   walk(std::false_type{});
   if (FMT == KV_SAME) {
@@ -969,7 +994,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
 
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    l[u] = groups_sum(l[u]);
+    l[u] = FMT == KV_SAME ? lsum[u][0] : groups_sum(l[u]);
     if (m[u] == -INFINITY && groups_umax(seen[u]) != 0) l[u] = NAN;
     const int row = wrow + 16 * u + col;
     if (16 * u + col >= wrows) continue;
