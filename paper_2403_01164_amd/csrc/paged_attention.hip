@@ -858,25 +858,29 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
 #pragma unroll
       for (int t = 0; t < KT; ++t) vs[t] *= to;
     }
-    float ms[U], al[U];
+    // The running maximum m only has to keep weights in range: it follows when a score passes it by
+    // more than 8 (weights of up to 2^8), so that the sums are seldom scaled.
+    float ms[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float mx = sc[0][u][0];
 #pragma unroll
       for (int e = 1; e < 4 * KT; ++e) mx = max_of(mx, sc[e >> 2][u][e & 3]);
-      mx = fmaxf(m[u], groups_max(mx) * mult[u]);
-      ms[u] = mx == -INFINITY ? 0.f : mx;
-      al[u] = exp2_hw(m[u] - ms[u]);
-      m[u] = mx;
-      l[u] *= al[u];
-      lsum[u] *= al[u];
-      if (FMT != KV_SAME) al[u] = __builtin_amdgcn_ldexpf(al[u], ve - e2);
-      if (__ballot(al[u] != 1.f)) {
+      mx = groups_max(mx) * mult[u];
+      if (__ballot(mx > m[u] + 8.f) || (FMT != KV_SAME && e2 != ve)) {
+        mx = fmaxf(m[u], mx);
+        float al = exp2_hw(m[u] - (mx == -INFINITY ? 0.f : mx));
+        m[u] = mx;
+        l[u] *= al;
+        lsum[u] *= al;
+        al = __builtin_amdgcn_ldexpf(al, ve - e2);
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) O[u][dt] *= al[u];
+        for (int dt = 0; dt < DT; ++dt) O[u][dt] *= al;
       }
+      ms[u] = m[u] == -INFINITY ? 0.f : m[u];
     }
     ve = e2;
+    __builtin_amdgcn_s_setprio(1);  // the other wavefront's vector work fits between these products
     f32x4 next[KT][U];
     score(next_keys, step + 1, next);
     // weights, rounded to 16 bits once: their errors average out over the positions
@@ -922,6 +926,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
         for (int u = 0; u < U; ++u) O[u][dt] = T::mfma(vf, pf[u][h], O[u][dt]);
       }
     }
+    __builtin_amdgcn_s_setprio(0);
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
