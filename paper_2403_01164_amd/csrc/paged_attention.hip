@@ -678,6 +678,9 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
   constexpr int KT = kManyKeys / 16;             // key tiles of a step
   constexpr int kSide = kManyKeys * D * 2;       // bytes of a step's keys (or values) in LDS
   constexpr int NL = kManyKeys * D * ES * 2 / 1024 / kManyWaves;  // loads of a step, per wavefront
+  // Scores are a step ahead of weights where there are registers for that: 8-bit pages on their way
+  // to LDS and their scales take them.  Keys come a step before their scores.
+  constexpr bool kAhead = FMT == KV_SAME;
   __shared__ __align__(16) char keys0[kSide], keys1[kSide], values0[kSide], values1[kSide];
   __shared__ float scales[2][FMT == KV_SAME ? 1 : 2 * kManyKeys];  // of keys, then of values, by step % 2
   __shared__ int s_odd;
@@ -807,11 +810,13 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
       *at = v;
     }
   };
-  // one step: sc are its scores, and the next step's (of next_keys) afterwards
-  auto compute = [&](const char* next_keys, const char* values, int step, Halves pg, f32x4(&sc)[KT][U], auto again) {
+  // one step.  kAhead: sc are its scores, and those of the next step's keys afterwards; otherwise
+  // its scores are computed here
+  auto compute = [&](const char* keys, const char* values, int step, Halves pg, f32x4(&sc)[KT][U], auto again) {
     constexpr bool careful = decltype(again)::value;
     const int jb = j0 + kManyKeys * step;
     if (jb > wmax) return;
+    if (!kAhead) score(keys, step, sc);
     const bool whole = pg.a >= 0 && pg.b >= 0 && jb + kManyKeys <= q.held;
     const bool full = whole && jb + kManyKeys - 1 <= wmin;
     // last position of either half that is in the cache
@@ -882,7 +887,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
     ve = e2;
     __builtin_amdgcn_s_setprio(1);  // the other wavefront's vector work fits between these products
     f32x4 next[KT][U];
-    score(next_keys, step + 1, next);
+    if (kAhead) score(keys, step + 1, next);
     // weights, rounded to 16 bits once: their errors average out over the positions
     u32x4 pf[U][KT / 2];
 #pragma unroll
@@ -927,10 +932,12 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
       }
     }
     __builtin_amdgcn_s_setprio(0);
+    if (kAhead) {
 #pragma unroll
-    for (int t = 0; t < KT; ++t)
+      for (int t = 0; t < KT; ++t)
 #pragma unroll
-      for (int u = 0; u < U; ++u) sc[t][u] = next[t][u];
+        for (int u = 0; u < U; ++u) sc[t][u] = next[t][u];
+    }
   };
 
   auto walk = [&](auto again) {
@@ -945,32 +952,35 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
       for (int dt = 0; dt < DT; ++dt) O[u][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     if (nsteps == 0) return;
-    // before step 0: its keys and values are in LDS, its scores known, the next keys on their way
+    // before step 0: its keys and values are in LDS (kAhead: its scores known, the next keys on their way)
     Halves pg0 = halves(0), pg1{-1, -1};
     issue(keys0, values0, 0, pg0);
     commit(keys0, values0, 0);
     if (nsteps > 1) pg1 = halves(1);
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    if (nsteps > 1 && side == 0) issue(keys1, values1, 1, pg1);
     f32x4 sc[KT][U];
-    score(keys0, 0, sc);
-    if (nsteps > 1 && side == 0) commit(keys1, values1, 1);
-    // a step: behind its barrier its values and the next keys are in LDS, and nobody reads the
-    // other two buffers, which take the keys after those and the next values
+    if (kAhead) {
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      if (nsteps > 1 && side == 0) issue(keys1, values1, 1, pg1);
+      score(keys0, 0, sc);
+    }
+    // a step: behind its barrier its values and keys (kAhead: the next keys) are in LDS, and nobody
+    // reads the other two buffers, which take the keys after those and the next values
+    const int lead = kAhead && side == 0 ? 2 : 1;
     auto turn = [&](char* next_keys, char* keys, char* values, char* next_values, int step) {
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();
       Halves pg2{-1, -1};
       if (step + 2 < nsteps) pg2 = halves(step + 2);
-      const bool more = step + 2 - side < nsteps;
-      if (more) issue(keys, next_values, step + 2 - side, side ? pg1 : pg2);
+      char* const to = kAhead ? keys : next_keys;
+      const bool more = step + lead < nsteps;
+      if (more) issue(to, next_values, step + lead, lead == 2 ? pg2 : pg1);
       if (pg0.a < 0 || pg0.b < 0 || j0 + kManyKeys * (step + 1) > q.held) {
         blank(values, step, pg0);
         __syncthreads();
       }
-      compute(next_keys, values, step, pg0, sc, again);
-      if (more) commit(keys, next_values, step + 2 - side);
+      compute(kAhead ? next_keys : keys, values, step, pg0, sc, again);
+      if (more) commit(to, next_values, step + lead);
       pg0 = pg1;
       pg1 = pg2;
     };
@@ -1144,9 +1154,11 @@ long long few_splits(PagedAttnParams* p, long long tiles, bool wide, long long r
   return heads * paged_most_items(cap, n_seq, p->tiles_each, heads, p->want, p->most);
 }
 
-// Workgroups that share a tile of the kernel for many rows.
+// Workgroups that share a tile of the kernel for many rows: kManyWorkgroups in all, counting the
+// tiles that the rows fill at least, and four steps each at least.
 int many_splits(const PagedCache& kv, const PagedSeqs& b, int heads) {
-  const long long tiles = paged_tiles(b, heads / kv.heads, kManyShift, 1) * kv.heads;
+  const long long rows = (long long)b.n_tokens * heads;
+  const long long tiles = (rows + (1 << kManyShift) - 1) >> kManyShift;
   const long long cap = (long long)b.max_pages << kv.page_shift;
   const long long most = std::min<long long>(kManyMaxSplits, (cap + 4 * kManyKeys - 1) / (4 * kManyKeys));
   return (int)std::max<long long>(1, std::min(most, kManyWorkgroups / tiles));
