@@ -1049,46 +1049,57 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
   }
 }
 
-// out = the joined partials of a row, one wavefront to a row.
+// out = the joined partials of a token's rows, a workgroup to a token, 4 dimensions to a thread.
+// Memory bounds it, and a chain of three round trips when there is little to join: the token's
+// sequence, the shares' (m, l), their sums.
 template <class A, int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p) {
-  constexpr int E = D / 64;
-  const int lane = threadIdx.x & 63;
-  const long long i = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (i >= (long long)p.seqs.n_tokens * p.heads) return;
-  const int token = (int)(i / p.heads), qhead = (int)(i % p.heads);
+  constexpr int kQuads = D / 4;
+  const int token = blockIdx.x;
   int local;
   PagedSeq q;
   if (paged_find(p.seqs, p.kv.page_shift, token, 1, 0, 0, &local, &q) < 0) return;
   const int t = token - q.row;
   if (t < 0 || t >= q.done || (long long)q.n * p.group <= p.min_rows) return;
-  // the tile's positions, as the kernel above shared them out
-  const int row = t * p.group + qhead % p.group;
-  const int tile0 = row >> kManyShift << kManyShift;
-  const int rows = min(q.done * p.group - tile0, 1 << kManyShift);
-  const int kend = max(min(q.held, q.first + (tile0 + rows - 1) / p.group + 1), 0);
-  int used;
-  many_share(kend, p.splits, &used);
-  if (used == 1) return;  // written already
-  const float* part = p.part + i * p.splits * D;
-  const float* ml = p.part + (long long)p.seqs.n_tokens * p.heads * p.splits * D + i * p.splits * 2;
-  float M = -INFINITY;
-  for (int k = 0; k < used; ++k) M = fmaxf(M, ml[2 * k]);
-  float L = 0.f, o[E] = {};
-  for (int k = 0; k < used; ++k) {
-    const float mk = ml[2 * k];
-    if (mk == -INFINITY) {
-      if (M == -INFINITY) L += ml[2 * k + 1];
-      continue;
+  const float* ml_all = p.part + (long long)p.seqs.n_tokens * p.heads * p.splits * D;
+  for (int i = threadIdx.x; i < p.heads * kQuads; i += 256) {
+    const int qhead = i / kQuads, d = i % kQuads * 4;
+    // the tile's positions, as the kernel above shared them out
+    const int tile0 = (t * p.group + qhead % p.group) >> kManyShift << kManyShift;
+    const int rows = min(q.done * p.group - tile0, 1 << kManyShift);
+    const int kend = max(min(q.held, q.first + (tile0 + rows - 1) / p.group + 1), 0);
+    int used;
+    many_share(kend, p.splits, &used);
+    if (used == 1) continue;  // written already
+    const long long at = ((long long)token * p.heads + qhead) * p.splits;
+    u32x2 ml[kManyMaxSplits];
+#pragma unroll
+    for (int k = 0; k < kManyMaxSplits; ++k)
+      ml[k] = k < used ? *(const u32x2*)(ml_all + (at + k) * 2) : u32x2{0xFF800000u, 0u};
+    float M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int k = 0; k < kManyMaxSplits; ++k) M = fmaxf(M, as_float(ml[k][0]));
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k0 = 0; k0 < kManyMaxSplits; k0 += 4) {
+      if (k0 >= used) break;
+      f32x4 part[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k0 + k < used) part[k] = *(const f32x4*)(p.part + (at + k0 + k) * D + d);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (k0 + k >= used) continue;
+        const bool none = as_float(ml[k0 + k][0]) == -INFINITY;
+        const float f = none ? 0.f : exp2_hw(as_float(ml[k0 + k][0]) - M), l = as_float(ml[k0 + k][1]);
+        L += none ? (M == -INFINITY ? l : 0.f) : f * l;
+        o += f * part[k];
+      }
     }
-    const float f = exp2_hw(mk - M);
-    L = fmaf(f, ml[2 * k + 1], L);
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(f, part[k * D + E * lane + e], o[e]);
+    o = L == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o / L;
+    *(u32x2*)((uint16_t*)p.out + (long long)token * p.ldo + qhead * D + d) =
+        u32x2{A::pack(o[0], o[1]), A::pack(o[2], o[3])};
   }
-  uint16_t* out = (uint16_t*)p.out + (long long)token * p.ldo + qhead * D + E * lane;
-#pragma unroll
-  for (int e = 0; e < E; ++e) out[e] = A::from_f32(L == 0.f ? 0.f : o[e] / L);
 }
 
 template <class A, int FMT, int D>
@@ -1114,8 +1125,7 @@ hipError_t many_t(const PagedAttnParams& p, const dim3& grid, hipStream_t st) {
   hipLaunchKernelGGL((paged_many_kernel<A, FMT, D>), grid, dim3(64 * kManyWaves), 0, st, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  const long long rows = (long long)p.seqs.n_tokens * p.heads;
-  hipLaunchKernelGGL((paged_join_kernel<A, D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, p);
+  hipLaunchKernelGGL((paged_join_kernel<A, D>), dim3((unsigned)p.seqs.n_tokens), dim3(256), 0, st, p);
   return hipGetLastError();
 }
 
