@@ -661,6 +661,7 @@ constexpr int kManyShift = 7;  // rows per tile: 128
 constexpr int kManyKeys = 64;  // positions at a time
 constexpr int kManyMaxSplits = 16;
 constexpr int kManyWorkgroups = 512;  // two for each of the 256 CUs
+constexpr long long kMaxManyPartials = 2LL * kManyWorkgroups << kManyShift;  // rows of all shares
 
 // Shares of a tile's positions [0, kend): `per` steps of kManyKeys each, *used of them.
 __device__ __forceinline__ int many_share(int kend, int splits, int* used) {
@@ -1164,14 +1165,18 @@ long long few_splits(PagedAttnParams* p, long long tiles, bool wide, long long r
   return heads * paged_most_items(cap, n_seq, p->tiles_each, heads, p->want, p->most);
 }
 
-// Workgroups that share a tile of the kernel for many rows: kManyWorkgroups in all, counting the
-// tiles that the rows fill at least, and four steps each at least.
-int many_splits(const PagedCache& kv, const PagedSeqs& b, int heads) {
-  const long long rows = (long long)b.n_tokens * heads;
-  const long long tiles = (rows + (1 << kManyShift) - 1) >> kManyShift;
+// Workgroups that share a tile of the kernel for many rows: no more than kManyWorkgroups in all, as
+// those run at a time, and four steps each at least.  The tiles are taken to be those of one
+// sequence, with a token of each other one left to the kernel for few rows when that runs, too.  513
+// tokens over 9217 positions, 32 heads on 8 (17 tiles of 8 heads): 3 shares 119 us, 4 144; 1024 tokens
+// over 3000 beside 23 single ones, heads of 64, int8 (32 tiles): 1 share 95 us, 2 80.
+int many_splits(const PagedCache& kv, const PagedSeqs& b, int heads, bool few) {
+  const long long rows = (long long)std::max(1, b.n_tokens - (few ? b.n_seq - 1 : 0)) * (heads / kv.heads);
+  const long long tiles = ((rows + (1 << kManyShift) - 1) >> kManyShift) * kv.heads;
   const long long cap = (long long)b.max_pages << kv.page_shift;
   const long long most = std::min<long long>(kManyMaxSplits, (cap + 4 * kManyKeys - 1) / (4 * kManyKeys));
-  return (int)std::max<long long>(1, std::min(most, kManyWorkgroups / tiles));
+  const long long room = kMaxManyPartials / ((long long)b.n_tokens * heads);
+  return (int)std::max<long long>(1, std::min({most, room, kManyWorkgroups / tiles}));
 }
 
 }  // namespace
@@ -1181,8 +1186,7 @@ size_t paged_ws_bytes(const PagedCache& kv, const PagedSeqs& b, int heads) {
   const long long chunks = std::min<long long>((cap + 127) / 128, kPagedMaxSplits);
   const long long rows = (long long)b.n_tokens * heads;
   const long long few = std::min(rows * chunks, kMaxPartials);
-  // a split tile is one of at most kManyWorkgroups, of 128 rows
-  const long long many = std::min<long long>(rows * kManyMaxSplits, (long long)kManyWorkgroups << kManyShift);
+  const long long many = std::min(rows * kManyMaxSplits, kMaxManyPartials);
   return kPagedCounters * sizeof(uint32_t) + (size_t)std::max(few, many) * (kv.head_dim + 2) * sizeof(float);
 }
 
@@ -1208,7 +1212,7 @@ hipError_t launch_paged_attention(PagedAttnParams p, double scale, void* ws, hip
     e = p.kv.dtype == 1 ? few_a<BF16>(p, wide, items, stream) : few_a<F16>(p, wide, items, stream);
   }
   if (e == hipSuccess && many) {
-    p.splits = many_splits(p.kv, b, p.heads);
+    p.splits = many_splits(p.kv, b, p.heads, few);
     p.min_rows = few ? kFewRows : 0;
     const dim3 grid((unsigned)(paged_tiles(b, p.group, kManyShift, 1) * p.kv.heads), (unsigned)p.splits);
     e = p.kv.dtype == 1 ? many_a<BF16>(p, grid, stream) : many_a<F16>(p, grid, stream);
