@@ -546,8 +546,8 @@ typedef struct {
  * read or written.  One sequence's pages may be another's, too (a common beginning), but for
  * pages that a write of the same call goes to. */
 typedef struct {
-  int n_tokens;              /* rows, in [0, 2^22]; n_tokens * heads < 2^28 */
-  int n_seq;                 /* in [0, 2^20] */
+  int n_tokens;              /* rows, in [0, 2^22]; n_tokens * heads <= 2^27 */
+  int n_seq;                 /* in [0, 2^20]; n_seq * heads <= 2^21 */
   int max_new;               /* most new tokens of any sequence, >= 1 */
   int max_pages;             /* columns of the table, >= 1; max_pages * page_size <= 2^30 */
   const int32_t* new_start;  /* [n_seq + 1] */

@@ -2689,7 +2689,8 @@ namespace {
 constexpr int kPagedMaxHeads = 1024;
 constexpr long long kPagedMaxPositions = 1LL << 30;
 constexpr int kPagedMaxTokens = 1 << 22, kPagedMaxSeqs = 1 << 20;
-constexpr long long kPagedMaxRows = 1LL << 28;  // n_tokens * heads
+// n_tokens * heads and n_seq * heads: the launches' grids stay below 2^32 threads
+constexpr long long kPagedMaxRows = 1LL << 27, kPagedMaxSeqRows = 1LL << 21;
 
 // fail(), also for calls without a context: their arguments are judged like any other's.
 template <class... Args>
@@ -2731,8 +2732,9 @@ const char* paged_batch(const hetegen_paged_batch* b, const hg::PagedCache& kv, 
   if (heads < 1 || heads > kPagedMaxHeads || heads % kv.heads)
     return "query heads: a multiple of the cache's heads, at most 1024";
   if (b->n_tokens < 0 || b->n_tokens > kPagedMaxTokens) return "n_tokens outside [0, 2^22]";
-  if ((long long)b->n_tokens * heads >= kPagedMaxRows) return "n_tokens * heads not below 2^28";
+  if ((long long)b->n_tokens * heads > kPagedMaxRows) return "n_tokens * heads above 2^27";
   if (b->n_seq < 0 || b->n_seq > kPagedMaxSeqs) return "n_seq outside [0, 2^20]";
+  if ((long long)b->n_seq * heads > kPagedMaxSeqRows) return "n_seq * heads above 2^21";
   if (b->max_new < 1) return "max_new below 1";
   if (b->max_pages < 1 || (long long)b->max_pages * kv.page_size > kPagedMaxPositions)
     return "max_pages below 1, or max_pages * page_size above 2^30";

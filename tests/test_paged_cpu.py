@@ -93,6 +93,15 @@ def test_refused_batches(over, status):
     assert _statuses(_kv(), _batch(**over), n=1 << 40) == (status,) * 3
 
 
+def test_refused_products():
+    kv = _kv(heads=1024)
+    big = dict(ld=1 << 16, heads=1024, ldq=1 << 16, ldo=1 << 16, n=1 << 40)
+    for over in (dict(n_tokens=2 ** 17 + 1), dict(n_seq=2 ** 11 + 1)):
+        assert _statuses(kv, _batch(**over), **big) == (INVALID,) * 3
+        assert hg.hetegen_paged_attention_ws_bytes(kv, _batch(**over), 1024) == 0
+    assert hg.hetegen_paged_attention_ws_bytes(kv, _batch(n_tokens=2 ** 17, n_seq=2 ** 11), 1024) > 0
+
+
 def test_refused_rows_and_workspaces():
     lib, kv, b = hg._lib, _kv(), _batch()
     for args, want in ((dict(k=0), INVALID), (dict(v=0), INVALID), (dict(k=4098), UNSUPPORTED),
@@ -117,11 +126,11 @@ def test_refused_rows_and_workspaces():
 
 def test_workspace_does_not_shrink():
     kv = _kv(head_dim=128)
-    for name, sizes in (("n_tokens", [0, 1, 2, 8, 100, 5000, 100000]), ("n_seq", [0, 1, 5, 300, 5000]),
+    for name, sizes in (("n_tokens", [0, 1, 2, 8, 100, 5000, 100000]), ("n_seq", [0, 1, 5, 300, 5000, 65536]),
                         ("max_new", [1, 2, 9, 100, 4000]), ("max_pages", [1, 2, 17, 1000, 100000])):
         got = [hg.hetegen_paged_attention_ws_bytes(kv, _batch(**{name: n}), 32) for n in sizes]
         assert got == sorted(got) and got[0] >= 262144, (name, got)
-    assert max(hg.hetegen_paged_attention_ws_bytes(kv, _batch(n_tokens=t, n_seq=t, max_pages=2 ** 25), 32)
+    assert max(hg.hetegen_paged_attention_ws_bytes(kv, _batch(n_tokens=t, n_seq=min(t, 65536), max_pages=2 ** 25), 32)
                for t in (1, 64, 4000, 10 ** 6)) < 200 << 20
 
 
