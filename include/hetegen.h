@@ -523,8 +523,8 @@ HETEGEN_API hetegen_status hetegen_decode_step_kv(hetegen_ctx* ctx, hetegen_mode
 
 typedef enum {
   HETEGEN_KV_SAME = 0, /* values as they are, in the cache's dtype */
-  HETEGEN_KV_I8 = 1,   /* code = round(x / c), half to even, c = max |x| / 127 over the head */
-  HETEGEN_KV_E4M3 = 2  /* OCP e4m3 of x / c, c = max |x| / 448 */
+  HETEGEN_KV_I8 = 1,   /* code = round(x / c), half to even, c = max |x| * (1 / 127) over the head */
+  HETEGEN_KV_E4M3 = 2  /* OCP e4m3 of x / c, c = max |x| * (1 / 448); all in binary32 */
 } hetegen_kv_format;
 
 typedef struct {

@@ -41,7 +41,7 @@ def quantise(bits, dtype, fmt):
     """Rows [..., D] of 16-bit patterns -> (codes as uint8 patterns, scales float32)."""
     x = decode(bits, dtype).astype(np.float32)
     with np.errstate(all="ignore"):
-        c = (np.max(np.abs(x), axis=-1) / QMAX[fmt]).astype(np.float32)
+        c = (np.max(np.abs(x), axis=-1) * (np.float32(1) / QMAX[fmt])).astype(np.float32)
         q = (x / np.where(c == 0, np.float32(1), c)[..., None]).astype(np.float32)
         ok = (np.isfinite(c) & (c > 0))[..., None]
         q = np.where(ok, q, np.float32(0))

@@ -1,8 +1,8 @@
 // Writing a paged KV cache and reading it back, on gfx950.
 //
 // write, 16-bit: the row is stored as it is.  8-bit, for each token and head, keys and values
-// apart: c = max_d |x_d| / Q (Q = 127 for int8, 448 for e4m3), code_d = round(x_d / c), half to
-// even, in binary32; c is kept as binary32.  A row of zeros has c = 0; a row that holds an
+// apart: c = max_d |x_d| * (1 / Q) (Q = 127 for int8, 448 for e4m3; 1 / Q rounded to binary32),
+// code_d = round(x_d / c), half to even, in binary32; c is kept as binary32.  A row of zeros has c = 0; a row that holds an
 // infinity or a NaN has c infinite or NaN and codes 0, so that it reads back as NaN and the
 // matrix products that multiply its codes with weights of 0 stay finite.
 // read: code_d * c, rounded once to the 16-bit type (half to even).
@@ -101,7 +101,7 @@ __device__ __forceinline__ float row_scale(const Row<D>& r) {
       const uint32_t w = r.x[i][j] & 0x7FFF7FFFu;
       m = max(m, max(w & 0xFFFFu, w >> 16));
     }
-  return T::to_f32(groups_umax(m)) / Quant<T, FMT>::kMax;
+  return T::to_f32(groups_umax(m)) * (1.f / Quant<T, FMT>::kMax);
 }
 
 // The 32 positions of a workgroup (see PagedTile), its position in the page and its record there
