@@ -216,18 +216,34 @@ __device__ __forceinline__ bool few_item(const PagedAttnParams& p, int w, FewIte
   const int tiles = lane < b.n_seq ? paged_few_tiles(q, p.group, p.min_rows, p.max_rows, R) : 0;
   const int unit = paged_unit(wave_sum(tiles * ((q.held + 127) >> 7)), p.kv.heads, p.want);
   const PagedPieces piece = paged_pieces(q.held, unit, p.most);
-  const int items = tiles * piece.count;
+  // the first pieces of all tiles come first, then the second ones: c is the piece with no more
+  // than w items in all pieces before it
+  int c = 0, before = 0;
+  if (b.n_seq > 1) {
+#pragma unroll
+    for (int bit = kPagedMaxSplits / 2; bit > 0; bit >>= 1) {
+      const int n = wave_sum(tiles * min(piece.count, c + bit));
+      if (n <= w) {
+        c += bit;
+        before = n;
+      }
+    }
+  } else {
+    const int t = __builtin_amdgcn_readfirstlane(tiles);
+    c = t > 0 ? w / t : 0;
+    before = c * t;
+  }
+  const int items = piece.count > c ? tiles : 0;
   const int upto = wave_scan(items);  // of this sequence and those before it
-  const uint64_t behind = __ballot(upto > w);
+  const uint64_t behind = __ballot(upto > w - before);
   if (!behind) return false;
   const int s = __builtin_ctzll(behind);
-  const int local = w - __builtin_amdgcn_readlane(upto - items, s), t = __builtin_amdgcn_readlane(tiles, s);
   it->s = s;
   it->q = PagedSeq{__builtin_amdgcn_readlane(q.row, s), __builtin_amdgcn_readlane(q.n, s),
                    __builtin_amdgcn_readlane(q.done, s), __builtin_amdgcn_readlane(q.first, s),
                    __builtin_amdgcn_readlane(q.held, s)};
-  it->tile = local % t;
-  it->chunk = local / t;
+  it->tile = w - before - __builtin_amdgcn_readlane(upto - items, s);
+  it->chunk = c;
   it->size = __builtin_amdgcn_readlane(piece.size, s);
   it->counter = (uint32_t)(s * p.tiles_each + it->tile);
   return true;

@@ -42,7 +42,7 @@ struct Quant {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float y = f[i] * r;
-        f[i] = fmaf(fmaf(-y, c, f[i]), r, y);
+        f[i] = copysignf(fmaf(fmaf(-y, c, f[i]), r, y), f[i]);  // (the correction loses the sign of -0)
       }
     } else {
 #pragma unroll

@@ -5,7 +5,9 @@
 #include <stdlib.h>
 
 #include <algorithm>
+#include <map>
 #include <random>
+#include <tuple>
 #include <vector>
 
 #include "../../paper_2403_01164_amd/csrc/paged.h"
@@ -40,7 +42,7 @@ static int find(const PagedSeqs& b, int tile, int unit, int shift, int extra, in
 int main() {
   std::mt19937 rng(7);
   auto pick = [&](int lo, int hi) { return std::uniform_int_distribution<int>(lo, hi)(rng); };
-  for (g_case = 0; g_case < 4000; ++g_case) {
+  for (g_case = 0; g_case < 3000; ++g_case) {
     const bool sound = g_case % 4 != 0;
     const int shift = 5 + pick(0, 3), page = 1 << shift;
     PagedSeqs b{};
@@ -146,6 +148,48 @@ int main() {
       }
     }
     CHECK(items <= paged_most_items(cap_b, b.n_seq, each, heads, want, most));
+
+    // the kernel's numbering: every (sequence, tile, piece) is one item, and items past the last none
+    const int unit = paged_unit(total, heads, want);
+    std::vector<int> tiles(b.n_seq), count(b.n_seq);
+    std::map<std::tuple<int, int, int>, int> seen;
+    for (int i = 0; i < b.n_seq; ++i) {
+      const PagedSeq q = paged_seq(b.start[i], b.start[i + 1], b.len[i], b, shift);
+      tiles[i] = paged_few_tiles(q, group, 0, max_rows, R);
+      count[i] = paged_pieces(q.held, unit, most).count;
+    }
+    if (items > 20000) continue;
+    for (int w = 0; w < items + 70; ++w) {
+      int c = 0, before = 0;
+      auto upto_piece = [&](int n) {
+        long long sum = 0;
+        for (int i = 0; i < b.n_seq; ++i) sum += (long long)tiles[i] * std::min(count[i], n);
+        return sum;
+      };
+      if (b.n_seq > 1) {
+        for (int bit = kPagedMaxSplits / 2; bit > 0; bit >>= 1)
+          if (upto_piece(c + bit) <= w) {
+            c += bit;
+            before = (int)upto_piece(c);
+          }
+      } else {
+        c = tiles[0] > 0 ? w / tiles[0] : 0;
+        before = c * tiles[0];
+      }
+      int upto = 0, found = -1, local = 0;
+      for (int i = 0; i < b.n_seq && found < 0; ++i) {
+        const int n = count[i] > c ? tiles[i] : 0;
+        if (upto + n > w - before) {
+          found = i;
+          local = w - before - upto;
+        }
+        upto += n;
+      }
+      CHECK((found >= 0) == (w < items));
+      if (found < 0) continue;
+      CHECK(local >= 0 && local < tiles[found] && c < count[found]);
+      CHECK(++seen[std::make_tuple(found, local, c)] == 1);
+    }
   }
   printf("index check ok\n");
   return 0;

@@ -141,6 +141,24 @@ def test_rows_of_zeros_extremes_and_no_numbers(ctx, dtype, fmt):
     assert np.array_equal(r[2], x[2].reshape(2, 64))
 
 
+@pytest.mark.parametrize("fmt", [paged.I8, paged.E4M3])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_quotients_are_rounded_as_a_division_rounds(ctx, dtype, fmt):
+    # rows of every magnitude of the type, many with values on or next to half a step
+    b = Batch(_kv(dtype, fmt, 64, 64, heads=4), [1500], [1500], 18)
+    rng = np.random.default_rng(19)
+    lo, hi = (-24, 15) if dtype == 0 else (-133, 127)
+    e = rng.integers(lo, hi + 1, (1500, 4, 1))
+    x = rng.integers(-255, 256, (1500, 4, 64)) / 256.0 * 2.0 ** e
+    x[..., 0] = np.where(rng.random((1500, 4)) < 0.5, 254 / 256 * 2.0 ** e[..., 0], x[..., 0])
+    k = bits(x.reshape(1500, 256), dtype)
+    v = bits(rng.normal(size=(1500, 256)) * 2.0 ** rng.uniform(lo / 2, hi / 2, (1500, 1)), dtype)
+    fill = _fill(b)
+    got = _write(ctx, b, device(fill), k, v)
+    want = _expected_write(b, fill, k, v)
+    assert np.array_equal(got.reshape(want.bytes.shape), want.bytes)
+
+
 @pytest.mark.parametrize("fmt", [paged.SAME, paged.I8, paged.E4M3])
 def test_missing_pages_positions_below_zero_and_behind_the_table(ctx, fmt):
     # sequence 0: pages that do not exist; 1: more new tokens than positions; 2: longer than the
