@@ -236,12 +236,30 @@ __global__ __launch_bounds__(kThreads) void paged_read_kernel(PagedCopyParams p)
   const int half = wave & 1, pos = lane & 15, g = lane >> 4, i = 16 * half + pos;
   const bool mine = i >= t.lo && i < t.hi;
   const long long P = p.kv.page_size;
-  Row<D> r;
+  constexpr int kLoads = D * ES / 64;                    // of a position's keys
+  constexpr int kChunks = kTile * D * ES / 16 / kThreads;  // of the tile's values, per thread
+  static_assert(kChunks * kThreads * 16 == kTile * D * ES || D * ES == 64, "values");
+  u32x4 kw[kLoads], vw[kChunks > 0 ? kChunks : 1];
+  float c = 1.f;
   if (t.rec) {
+    // everything that the tile needs is requested at once
+    const char* kdata = t.rec + (long long)t.off * D * ES + half * (16 * D * ES) + lane * 16;
     const char* vdata = t.rec + P * D * ES + (long long)t.off * D * ES;
-    for (int u = threadIdx.x; u < kTile * D * ES / 16; u += kThreads) {
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k)
+      if (!values) kw[k] = load16_nt(kdata + k * 1024);
+    if (FMT != KV_SAME) c = ((const float*)(t.rec + 2 * P * D) + (values ? P : 0) + t.off)[i];
+#pragma unroll
+    for (int n = 0; n < (kChunks > 0 ? kChunks : 1); ++n) {
+      const int u = threadIdx.x + n * kThreads;
+      if (u < kTile * D * ES / 16) vw[n] = load16_nt(vdata + u * 16);
+    }
+#pragma unroll
+    for (int n = 0; n < (kChunks > 0 ? kChunks : 1); ++n) {
+      const int u = threadIdx.x + n * kThreads;
+      if (u >= kTile * D * ES / 16) continue;
       const int l = u & 63, d0 = (u >> 6) * (16 * 2 / ES) + (l & 15), vg = l >> 4;
-      const u32x4 w = load16_nt(vdata + u * 16);
+      const u32x4 w = vw[n];
       if (FMT == KV_SAME) {
 #pragma unroll
         for (int x = 0; x < 8; ++x)
@@ -256,24 +274,21 @@ __global__ __launch_bounds__(kThreads) void paged_read_kernel(PagedCopyParams p)
   }
   __syncthreads();
   if (!mine) return;
-  float c = 1.f;
-  if (FMT != KV_SAME && t.rec) c = ((const float*)(t.rec + 2 * P * D) + (values ? P : 0) + t.off)[i];
-  const char* src = t.rec + (long long)t.off * D * ES + half * (16 * D * ES) + lane * 16;
-#pragma unroll
-  for (int k = 0; k < D / 32; ++k) {
-    if (!t.rec) {
-      r.x[k] = u32x4{0u, 0u, 0u, 0u};
-    } else if (FMT == KV_SAME) {
-      r.x[k] = values ? *(const u32x4*)(lds + i * RS + (32 * k + 8 * g) * ES) : load16_nt(src + k * 1024);
-    } else {
-      const u32x2 w = values ? *(const u32x2*)(lds + i * RS + 32 * k + 8 * g)
-                             : *(const u32x2*)(src + (k >> 1) * 1024 + (k & 1) * 8);
-      r.x[k] = Quant<T, FMT>::values(w, c);
-    }
-  }
   uint16_t* dst = (uint16_t*)(values ? p.v : p.k) + (long long)(t.row + i) * p.ld + head * D + 8 * g;
 #pragma unroll
-  for (int k = 0; k < D / 32; ++k) *(u32x4*)(dst + 32 * k) = r.x[k];
+  for (int k = 0; k < D / 32; ++k) {
+    u32x4 x = {0u, 0u, 0u, 0u};
+    if (t.rec) {
+      if (FMT == KV_SAME) {
+        x = values ? *(const u32x4*)(lds + i * RS + (32 * k + 8 * g) * ES) : kw[k];
+      } else {
+        const u32x4& w = kw[k >> 1];
+        x = Quant<T, FMT>::values(values ? *(const u32x2*)(lds + i * RS + 32 * k + 8 * g)
+                                         : u32x2{w[2 * (k & 1)], w[2 * (k & 1) + 1]}, c);
+      }
+    }
+    *(u32x4*)(dst + 32 * k) = x;
+  }
 }
 
 template <class T, int FMT, int D>
