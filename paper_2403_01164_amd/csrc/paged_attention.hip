@@ -19,7 +19,7 @@
 // two per row, taken back in the score's factor, keeps bf16 queries in range, exactly unless a value
 // is 2^29 times smaller than its row's largest).  A key's scale multiplies its score; a value's
 // scale multiplies its weight, relative to a power of two per wavefront that follows the largest
-// scale seen, so that the product stays in [0, 1].
+// scale seen, so that the product is no larger than the weight.
 #include "paged_device.h"
 
 #include <math.h>
@@ -1156,9 +1156,11 @@ hipError_t many_a(const PagedAttnParams& p, const dim3& grid, hipStream_t st) {
   return wide ? many_t<A, KV_E4M3, 128>(p, grid, st) : many_t<A, KV_E4M3, 64>(p, grid, st);
 }
 
-// A sequence's rows per key/value head (new tokens x heads of the group) up to which it goes to
-// the kernel for few rows when a batch needs both.
-constexpr int kFewRows = 32;
+// A sequence's rows per key/value head (new tokens x heads of the group) up to which the kernel for few
+// rows takes it.  16 sequences of 2500 positions, 8 heads of 128: at 36 rows 45 us (the other kernel
+// 62), at 64 rows 44 (55), at 96 rows 64 (60); four sequences with a key head per query head: 48 rows
+// 40 (50), 90 rows 59 (54).
+constexpr int kFewRows = 64;
 
 // How the kernel for few rows deals a batch: as many pieces as workgroups run at a time on 256
 // CUs (their registers allow 2 to 4 on each), as far as the partials (kMaxPartials rows of all

@@ -131,9 +131,9 @@ int main() {
     if (b.n_seq > kPagedDense || b.n_tokens == 0) continue;
     const int group = pick(1, 4), R = pick(0, 1) ? 16 : 32, cap_b = b.max_pages * page;
     const bool limited = pick(0, 1);  // the kernel for many rows takes the others
-    const int max_rows = limited ? 32 : 0x7FFFFFFF;
+    const int max_rows = limited ? 64 : 0x7FFFFFFF;
     const long long longest = (long long)std::min(b.max_new, b.n_tokens) * group;
-    const int each = (int)((std::min<long long>(longest, limited ? 32 : longest) + R - 1) / R);
+    const int each = (int)((std::min<long long>(longest, limited ? 64 : longest) + R - 1) / R);
     long long total = 0, items = 0;
     for (int pass = 0; pass < 2; ++pass) {
       const int unit = paged_unit(total, heads, want);
