@@ -214,7 +214,8 @@ __device__ __forceinline__ bool few_item(const PagedAttnParams& p, int w, FewIte
   const int st = load_i32(b.start + i);
   const PagedSeq q = paged_seq(st, load_i32(b.start + i + 1), load_i32(b.len + i), b, p.kv.page_shift);
   const int tiles = lane < b.n_seq ? paged_few_tiles(q, p.group, p.min_rows, p.max_rows, R) : 0;
-  const int unit = paged_unit(wave_sum(tiles * ((q.held + 127) >> 7)), p.kv.heads, p.want);
+  // (at most 4 tiles of 2^23 units for each of 64 sequences)
+  const int unit = paged_unit(wave_sum((uint32_t)tiles * ((q.held + 127) >> 7)), p.kv.heads, p.want);
   const PagedPieces piece = paged_pieces(q.held, unit, p.most);
   // the first pieces of all tiles come first, then the second ones: c is the piece with no more
   // than w items in all pieces before it
@@ -222,7 +223,7 @@ __device__ __forceinline__ bool few_item(const PagedAttnParams& p, int w, FewIte
   if (b.n_seq > 1) {
 #pragma unroll
     for (int bit = kPagedMaxSplits / 2; bit > 0; bit >>= 1) {
-      const int n = wave_sum(tiles * min(piece.count, c + bit));
+      const int n = (int)wave_sum((uint32_t)(tiles * min(piece.count, c + bit)));
       if (n <= w) {
         c += bit;
         before = n;
@@ -1222,7 +1223,8 @@ hipError_t launch_paged_attention(PagedAttnParams p, double scale, void* ws, hip
   const bool many = longest > kFewRows, few = !many || shortest <= kFewRows;
   hipError_t e = hipSuccess;
   if (few) {
-    const bool wide = longest > 16;
+    // (beside a kernel for many rows it is single tokens, as a rule)
+    const bool wide = (many ? p.group : longest) > 16;
     const long long tiles = paged_tiles(b, p.group, wide ? kFewShift<2> : kFewShift<1>, 1) * p.kv.heads;
     const unsigned items = (unsigned)few_splits(&p, tiles, wide, std::min(longest, (long long)kFewRows));
     p.min_rows = 0;

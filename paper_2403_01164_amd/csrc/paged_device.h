@@ -85,13 +85,13 @@ __device__ __forceinline__ float groups_sum(float v) {
   return over_groups(v, [](float x, float y) { return x + y; });
 }
 
-// Sum over the wavefront, in every lane.
-__device__ __forceinline__ int wave_sum(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, false);   // lane ^ 1
-  v += __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, false);   // lane ^ 2
-  v += __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, false);  // mirrored half row
-  v += __builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, false);  // mirrored row of 16
-  return __builtin_amdgcn_readfirstlane((int)over_groups((uint32_t)v, [](uint32_t x, uint32_t y) { return x + y; }));
+// Sum over the wavefront, in every lane (below 2^32).
+__device__ __forceinline__ uint32_t wave_sum(uint32_t v) {
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false);   // lane ^ 1
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false);   // lane ^ 2
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, false);  // mirrored half row
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, false);  // mirrored row of 16
+  return __builtin_amdgcn_readfirstlane(over_groups(v, [](uint32_t x, uint32_t y) { return x + y; }));
 }
 
 // Sum over the lanes up to this one.
