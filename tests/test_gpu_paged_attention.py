@@ -212,6 +212,34 @@ def test_one_sequence_in_many_and_shared_pages(ctx):
     _run(ctx, b, 2, seed=26)
 
 
+@pytest.mark.parametrize("dtype,fmt,D", [(0, paged.SAME, 128), (1, paged.I8, 64), (1, paged.SAME, 64), (0, paged.E4M3, 128)])
+def test_more_sequences_than_a_wavefront_numbers(ctx, dtype, fmt, D):
+    # over 64 sequences: long and short ones, one token, a few, chunks and none
+    n = 70
+    lens = [1 + (61 * i) % 400 + (5000 if i % 23 == 5 else 0) for i in range(n)]
+    new = [min(l, (0, 1, 1, 2, 5)[i % 5]) for i, l in enumerate(lens)]
+    _run(ctx, Batch(_kv(dtype, fmt, D, 64, heads=1), lens, new, 47, lead=1, tail=1), 2, seed=34)
+    new[5], new[60] = 90, 70
+    lens[60] += 100
+    _run(ctx, Batch(_kv(dtype, fmt, D, 64, heads=1), lens, new, 48), 2, seed=35)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_batches_drawn_at_random(ctx, seed):
+    rng = np.random.default_rng(1000 + seed)
+    fmt = int(rng.integers(0, 3))
+    kv_heads, group = int(rng.integers(1, 5)), int(rng.choice([1, 2, 3, 4, 7]))
+    n_seq = int(rng.choice([1, 2, 3, 7, 20]))
+    budget = 500 // (n_seq * group)
+    new = [int(rng.integers(0, 4)) if rng.random() < 0.6 else int(rng.integers(1, max(2, budget))) for _ in range(n_seq)]
+    lens = [n + int(rng.choice([0, 1, 40, 500, 3000]) * rng.random()) for n in new]
+    b = Batch(_kv(int(rng.integers(0, 2)), fmt, int(rng.choice([64, 128])), int(rng.choice([32, 64, 128, 256])), heads=kv_heads),
+              lens, new, seed, lead=int(rng.integers(0, 3)), tail=int(rng.integers(0, 3)))
+    if b.T == 0 or sum(new) == 0:
+        b = Batch(b.kv, [9], [2], seed)
+    _run(ctx, b, kv_heads * group, seed=2000 + seed)
+
+
 def test_unsound_offsets_stay_inside(ctx):
     b = Batch(_kv(0, paged.SAME, 64, 32), [90, 60, 45], [30, 30, 30], 37)
     pages, ws = device(_stored(b, 27).bytes), workspace(b, 4)
