@@ -183,6 +183,8 @@ __device__ __forceinline__ float over_lanes(float v, F op) {
 // 1 KiB a load, and feed U products.  The wavefronts' sums meet in LDS; a sequence of several
 // chunks leaves partials [m, l, o] in the workspace and the last workgroup of (tile, head) to arrive
 // joins them in chunk order (an arrival counter, no waiting), so results do not depend on timing.
+// Memory bounds it, and a fixed part of each launch: 8 sequences over 16000 positions, 40 heads of
+// 128, int8, 215 us (6.1 TB/s), over 4000 64 us (4.8); one sequence of 513, 32 heads, fp16, 8.6 us.
 constexpr int kFewWaves = 4;
 template <int U>
 constexpr int kFewShift = U == 2 ? 5 : 4;  // rows per tile: 16 U
@@ -672,7 +674,8 @@ __global__ __launch_bounds__(64 * kFewWaves, U == 2 ? 2 : D == 128 ? 3 : 4) void
 // LDS feeds two products.  The scores of the next step are computed beside the weights of this one,
 // so that matrix cores and vector units have work at the same time, and a step has one barrier.
 // When there are few tiles, several workgroups share a tile's positions and a second kernel joins
-// their partials.
+// their partials.  The softmax's vector work beside the products bounds it: prompts of 2048 and 7000
+// tokens, 32 heads of 128, bf16, 464 to 505 us (863 to 939 TFLOP/s; a large library product 1214).
 constexpr int kManyWaves = 4;
 constexpr int kManyShift = 7;  // rows per tile: 128
 constexpr int kManyKeys = 64;  // positions at a time
@@ -1069,7 +1072,7 @@ __global__ __launch_bounds__(64 * kManyWaves, 2) void paged_many_kernel(PagedAtt
 
 // out = the joined partials of a token's rows, a workgroup to a token, 4 dimensions to a thread.
 // Memory bounds it, and a chain of three round trips when there is little to join: the token's
-// sequence, the shares' (m, l), their sums.
+// sequence, the shares' (m, l), their sums.  513 tokens of 32 heads of 128 in 3 shares: 9.0 us.
 template <class A, int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnParams p) {
   constexpr int kQuads = D / 4;

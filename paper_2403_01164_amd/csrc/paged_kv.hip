@@ -7,7 +7,9 @@
 // matrix products that multiply its codes with weights of 0 stay finite.
 // read: code_d * c, rounded once to the 16-bit type (half to even).
 //
-// Both move every byte once, so memory bounds them (the launch, for single tokens).  A workgroup
+// Both move every byte once, so memory bounds them (the launch, for single tokens): 65536 positions of
+// 40 heads of 128, int8, written in 469 us (4.3 TB/s) and read in 466 (4.4; a large copy reaches 4.83),
+// one token of 8 sequences, 16-bit, in 3.2 and 3.6.  A workgroup
 // takes the 32 positions of one value tile (two key tiles) of one head: wavefronts 0 and 1 the
 // keys, whose 16-byte pieces only change places, 2 and 3 the values, which pass through LDS to
 // bring 8 positions of one dimension together.  Lane (position, group of 8 dimensions) holds
