@@ -585,8 +585,9 @@ HETEGEN_API size_t hetegen_paged_attention_ws_bytes(const hetegen_paged_kv* kv, 
  * that have a page, K and V of key/value head h / (heads / kv->heads); 0 where there is none.
  * q_dev and out_dev [n_tokens, heads * head_dim] (device, kv->dtype, row strides ldq and ldo
  * elements, multiples of 8, 16-byte aligned, not overlapping).  heads is a multiple of kv->heads, at
- * most 1024; scale is finite (1 / sqrt(head_dim) as a rule).  Softmax and sums in binary32; keys
- * and values in masked places do not reach the result, whatever they are.
+ * most 1024; scale (1 / sqrt(head_dim) as a rule) is finite, in binary32 and times log2(e), too.
+ * Softmax and sums in binary32, whose range scaled scores have to keep to; keys and values in
+ * masked places do not reach the result, whatever they are.
  * ws_dev: hetegen_paged_attention_ws_bytes of device memory, 16-byte aligned, of which the first
  * 256 KiB are zero before its first use (every call leaves them zero); calls that overlap need a
  * workspace each.  Results do not depend on timing; their last bits may depend on the batch's sizes

@@ -2848,7 +2848,8 @@ hetegen_status hetegen_paged_attention(hetegen_ctx* ctx, const hetegen_paged_kv*
     TRY(paged_check(ctx, call, kv, pages_dev, batch, heads, {q_dev, out_dev}, &p.kv, &p.seqs));
     TRY(paged_stride(ctx, call, ldq, (long long)heads * p.kv.head_dim));
     TRY(paged_stride(ctx, call, ldo, (long long)heads * p.kv.head_dim));
-    if (!std::isfinite(scale)) return refuse(ctx, HETEGEN_ERR_INVALID_ARG, "%s: scale is not finite", call);
+    if (!std::isfinite((float)(scale * 1.4426950408889634)))  // the kernels multiply scores by scale * log2(e)
+      return refuse(ctx, HETEGEN_ERR_INVALID_ARG, "%s: scale * log2(e) is not finite in binary32", call);
     if (paged_empty(p.seqs)) return HETEGEN_OK;
     if (q_dev == out_dev) return refuse(ctx, HETEGEN_ERR_INVALID_ARG, "%s: q and out overlap", call);
     TRY(paged_workspace(ctx, call, ws_dev, ws_bytes, hg::paged_ws_bytes(p.kv, p.seqs, heads)));

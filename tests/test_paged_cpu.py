@@ -124,6 +124,14 @@ def test_refused_rows_and_workspaces():
     assert lib.hetegen_decode_step_paged_ws_bytes(None, kv, b) == 0
 
 
+@pytest.mark.parametrize("scale", [3.4e38, -3.4e38, 1e300, -1e300])
+def test_scales_that_binary32_cannot_hold_are_refused(scale):
+    # scale * log2(e) is what multiplies scores; the misplaced workspace would be refused after it
+    assert _statuses(_kv(), _batch(), scale=scale, ws=4104)[2] == INVALID
+    for held in (2.3e38, -2.3e38, 0.0, 1e-300):
+        assert _statuses(_kv(), _batch(), scale=held, ws=4104)[2] == UNSUPPORTED
+
+
 def test_workspace_does_not_shrink():
     kv = _kv(head_dim=128)
     for name, sizes in (("n_tokens", [0, 1, 2, 8, 100, 5000, 100000]), ("n_seq", [0, 1, 5, 300, 5000, 65536]),
